@@ -5,4 +5,4 @@ Python module ``acp`` is a thin ctypes binding with the C ABI's names.  Nothing
 is loaded at import time: the library is opened on first use, and every entry
 point raises if it is missing.
 """
-__all__ = ["acp", "workloads"]
+__all__ = ["acp", "ops", "workloads"]

@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "acp_internal.h"
+#include "acp_ops.h"
 
 namespace {
 
@@ -208,22 +209,34 @@ acp_status acp_timing_reset(void) {
     return ok();
 }
 
-acp_status acp_timing_read(acp_kernel_times* out) {
-    if (out == nullptr) return fail(ACP_EINVAL, "out is NULL");
-    for (int k = 0; k < ACP_K_COUNT; ++k) {
-        out->launches[k] = 0;
-        out->ms[k] = 0.0;
+// Sums of the recorded kernels first .. first + count - 1
+static acp_status read_times(int first, int count, int64_t* launches, double* total) {
+    for (int k = 0; k < count; ++k) {
+        launches[k] = 0;
+        total[k] = 0.0;
     }
     for (const TraceRec& r : g_trace.recs) {
+        const int k = r.kernel - first;
+        if (k < 0 || k >= count) continue;
         hipError_t e = hipEventSynchronize(r.stop);
         if (e != hipSuccess) return hip_status(e, "acp_timing_read");
         float ms = 0.f;
         e = hipEventElapsedTime(&ms, r.start, r.stop);
         if (e != hipSuccess) return hip_status(e, "acp_timing_read");
-        out->launches[r.kernel] += 1;
-        out->ms[r.kernel] += ms;
+        launches[k] += 1;
+        total[k] += ms;
     }
     return ok();
+}
+
+acp_status acp_timing_read(acp_kernel_times* out) {
+    if (out == nullptr) return fail(ACP_EINVAL, "out is NULL");
+    return read_times(0, ACP_K_COUNT, out->launches, out->ms);
+}
+
+acp_status acp_op_timing_read(acp_op_times* out) {
+    if (out == nullptr) return fail(ACP_EINVAL, "out is NULL");
+    return read_times(ACP_K_COUNT, ACP_OP_COUNT, out->launches, out->ms);
 }
 
 acp_status acp_workspace_size(int B, int H, int L, int d, acp_dtype dt, size_t* bytes) {

@@ -1,0 +1,204 @@
+"""Norms and their gradients against the formulas in float64.
+
+Tolerances.  With e = 2^-24: a row's mean is off by at most 80 e mean|x| (each thread adds
+up to 32 features, then at most 12 levels of partial sums; 80 leaves room for the centred
+squares), a statistic by 80 e relative, and each elementwise step by a few e; outputs add
+half a step of their type.  A weight's gradient adds chains of up to 250 terms."""
+import pytest
+import torch
+
+from paper_2504_06949_amd import ops
+from tests._helpers import ensure_built
+
+pytestmark = pytest.mark.gpu
+E = 2.0 ** -24
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    ensure_built()
+
+
+def _half(t):
+    return torch.finfo(t).eps / 2
+
+
+def reference(x, w, b, eps, center, dy=None):
+    """(y, dx, dw, db) in float64 and their tolerances in units that exclude the type."""
+    x = x.double()
+    per_head = w.dim() == 2
+    w64 = w.double()[:, None, :] if per_head else w.double()
+    b64 = 0.0 if b is None else (b.double()[:, None, :] if per_head else b.double())
+    n = x.shape[-1]
+    m = x.mean(-1, keepdim=True) if center else torch.zeros_like(x[..., :1])
+    r = 1.0 / ((x - m).square().mean(-1, keepdim=True) + eps).sqrt()
+    xh = (x - m) * r
+    y = xh * w64 + b64
+    off = 80 * E * x.abs().mean(-1, keepdim=True) * r * (1.0 if center else 0.0)   # of xh, by the mean
+    ty = off * w64.abs() + 80 * E * (xh * w64).abs() + 4 * E * (b64.abs() if b is not None else 0.0)
+    if dy is None:
+        return y, ty
+    dy = dy.double()
+    g = dy * w64
+    m2 = (g * xh).mean(-1, keepdim=True)
+    m1 = g.mean(-1, keepdim=True) if center else torch.zeros_like(m2)
+    dx = r * (g - m1 - xh * m2)
+    a2 = (g * xh).abs().mean(-1, keepdim=True)
+    a1 = g.abs().mean(-1, keepdim=True)
+    tdx = r * (200 * E * (g.abs() + a1 + xh.abs() * a2) + 2 * off * (m2.abs() + xh.abs() * a1))
+    over = (0, 2) if per_head else tuple(range(x.dim() - 1))
+    dw, db = (dy * xh).sum(over), dy.sum(over)
+    tdw = 250 * E * (dy * xh).abs().sum(over) + (dy.abs() * off).sum(over)
+    return y, ty, dx, tdx, dw, tdw, db, 250 * E * dy.abs().sum(over)
+
+
+def close(got, want, tol, half):
+    err = (got.double() - want).abs()
+    lim = tol + half * want.abs() + 1e-30
+    bad = err > lim
+    assert not bad.any(), f"{int(bad.sum())} of {bad.numel()}, worst {float((err / lim).max()):.2f} of the limit"
+
+
+def check(x, w, b, center, eps=1e-5):
+    g = torch.Generator(device="cuda").manual_seed(5)
+    dy = torch.randn(x.shape, generator=g, device="cuda").to(x.dtype)
+    y, mean, rstd = ops.norm_forward(x, w, b, eps, center=center)
+    dx, dw, db = ops.norm_backward(dy, x, w, mean, rstd, bias=b is not None)
+    ref = reference(x, w, b, eps, center, dy)
+    h = _half(x.dtype)
+    close(y, ref[0], ref[1], h)
+    close(dx, ref[2], ref[3], h)
+    close(dw, ref[4], ref[5], E)
+    if b is not None:
+        close(db, ref[6], ref[7], E)
+    assert (mean is None) == (not center)
+    return y, dx, dw, db
+
+
+def _x(shape, dtype, seed=1, offset=0.5):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn(shape, generator=g, device="cuda") * 2 + offset).to(dtype)
+
+
+def _w(shape, dtype=torch.float32, seed=2):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn(shape, generator=g, device="cuda") * 0.3 + 1).to(dtype)
+
+
+# every thread layout (8 lanes to 1024 threads, 1 to 4 pieces), its last width and the next
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n", [1, 2, 7, 31, 32, 33, 64, 65, 127, 128, 129, 256, 257, 512, 513, 768, 1023, 1024,
+                               1025, 1537, 2048, 2049, 4095, 4096, 4097, 8192, 8193, 16384])
+def test_widths(n, dtype):
+    print(f"case: norm n={n} {dtype}", flush=True)
+    x, w, b = _x((37, n), dtype), _w(n), _w(n, seed=3)
+    check(x, w, b, True)
+    check(x, w, None, False)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("B,H,L,n", [(1, 1, 1, 64), (2, 3, 5, 64), (3, 12, 100, 64), (1, 7, 1, 128), (2, 5, 67, 96)])
+def test_a_weight_per_head_and_strided_rows(B, H, L, n, dtype):
+    print(f"case: norm per head {B} {H} {L} {n} {dtype}", flush=True)
+    fused = _x((B, L, 3, H, n), dtype)
+    w = _w((H, n), torch.bfloat16 if n == 64 else torch.float32)
+    x = fused[:, :, 1].transpose(1, 2)                   # [B, H, L, n], rows of a fused projection
+    y, dx, dw, _ = check(x, w, None, False)
+    y2, dx2, dw2, _ = check(x.contiguous(), w, None, False)
+    assert torch.equal(y, y2) and torch.equal(dx, dx2) and torch.equal(dw, dw2)
+    check(x, w, _w((H, n), w.dtype, 7), True)
+    check(x, w[0].contiguous(), None, False)             # one weight row for strided heads
+
+
+@pytest.mark.parametrize("rows,n", [(1, 768), (20000, 64), (5000, 768), (700, 4096)])
+def test_many_rows(rows, n):
+    print(f"case: norm rows={rows} n={n}", flush=True)
+    check(_x((rows, n), torch.bfloat16), _w(n, torch.bfloat16), _w(n, torch.bfloat16, 3), True)
+
+
+def test_repeated_runs_are_equal():
+    x, w = _x((3000, 320), torch.bfloat16), _w(320)
+    first = check(x, w, None, True)
+    for _ in range(3):
+        for a, b in zip(first[:3], check(x, w, None, True)[:3]):
+            assert torch.equal(a, b)
+
+
+def test_offset_rows_keep_their_precision():
+    """A mean 1000 times the deviation: the centred squares, not differences of squares."""
+    check(_x((50, 512), torch.float32, offset=2000.0), _w(512), None, True)
+
+
+def test_rows_of_zeros_constants_and_non_finite_rows():
+    x = _x((8, 200), torch.float32)
+    x[1] = 0.0
+    x[2] = 3.0
+    w, b = _w(200), _w(200, seed=3)
+    y, _, _ = ops.norm_forward(x, w, b, 1e-5, center=True)
+    assert torch.equal(y[1], b) and torch.isfinite(y).all()
+    close(y[2], b.double(), 400 * w.double().abs() * 80 * E * 3.0 / 1e-5 ** 0.5, E)
+    clean, _, _ = ops.norm_forward(x, w, b, 1e-5, center=True)
+    x[5, 7], x[6, 0] = float("inf"), float("nan")
+    y, _, _ = ops.norm_forward(x, w, b, 1e-5, center=True)
+    for r in range(8):
+        assert torch.isnan(y[r]).any() if r in (5, 6) else torch.equal(y[r], clean[r])
+
+
+@pytest.mark.parametrize("shape", [(0, 64), (2, 0, 3, 64)])
+def test_no_rows(shape):
+    x, w = torch.empty(shape, device="cuda"), _w(64)
+    y, mean, rstd = ops.norm_forward(x, w, None, center=True)
+    dx, dw, db = ops.norm_backward(torch.empty_like(x), x, w, mean, rstd, bias=True)
+    assert y.shape == x.shape and dx.shape == x.shape
+    assert not dw.any() and not db.any()
+
+
+def test_autograd():
+    """Gradients through layer_norm and rms_norm, of a broadcast input and a shared weight
+    among them, against float64 autograd of the formula; and against differences."""
+    x = _x((2, 3, 40, 64), torch.float32)
+    row = _x((1, 1, 1, 64), torch.float32, seed=9)
+    w, b = _w((3, 64)), _w((3, 64), seed=3)
+    leaves = [t.clone().requires_grad_(True) for t in (x, row, w, b)]
+    wide = [t.double().requires_grad_(True) for t in (x, row, w, b)]
+
+    def f(x, row, w, b, own):
+        def ln(t, w, b, eps=1e-5):
+            if own:
+                return ops.layer_norm(t, w, b, eps)
+            c = t - t.mean(-1, keepdim=True)
+            return c / (c.square().mean(-1, keepdim=True) + eps).sqrt() * w[:, None] + b[:, None]
+
+        def rms(t, w, eps=1e-6):
+            return ops.rms_norm(t, w, eps) if own else t / (t.square().mean(-1, keepdim=True) + eps).sqrt() * w[:, None]
+
+        t = ln(x + row, w, b)
+        return (rms(t.transpose(2, 3).contiguous().transpose(2, 3), w) + rms(row.expand(2, 3, 40, 64), w)).sin().sum()
+
+    f(*leaves, True).backward()
+    f(*wide, False).backward()
+    for a, r in zip(leaves, wide):
+        # (sums over up to 80 rows of differently rounded terms: a few hundred roundings)
+        assert (a.grad.double() - r.grad).abs().max() <= 1000 * E * r.grad.abs().max()
+    # differences in float32, of a step that moves the sum by much more than its rounding
+    d = torch.randn_like(x)
+    h = 1e-2
+    with torch.no_grad():
+        diff = (ops.layer_norm(x + h * d, w, b).double().sin().sum()
+                - ops.layer_norm(x - h * d, w, b).double().sin().sum()) / (2 * h)
+    y = x.clone().requires_grad_(True)
+    ops.layer_norm(y, w, b).double().sin().sum().backward()
+    slope = (y.grad.double() * d.double()).sum()
+    assert abs(float(diff - slope)) <= 1e-2 * float((y.grad.double() * d.double()).abs().sum()) ** 1.0 * 0.1
+
+
+def test_dx_in_place_of_dy_and_row_offsets_past_31_bits():
+    x, w = _x((64, 128), torch.bfloat16), _w(128)
+    check(x, w, None, False)
+    big = torch.empty((3, 1, 1 << 30), dtype=torch.bfloat16, device="cuda")   # rows 2^30 elements apart
+    rows = big[:, None, :, :128].expand(3, 1, 1, 128)
+    src = _x((3, 128), torch.bfloat16)
+    big[:, 0, :128] = src
+    y, _, _ = ops.norm_forward(rows, w)
+    want, _, _ = ops.norm_forward(src, w)
+    assert torch.equal(y.view(3, 128), want)
