@@ -25,6 +25,7 @@ namespace {
 
 constexpr int kShortRows = 16;    // rows of a short sequence: new tokens times query heads
 constexpr int kMaxSplit = 64;     // parts of a row's keys (a lane each in the merge)
+constexpr float kSlack = 8.f;     // a weight is at most 2^8
 
 __device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
@@ -52,17 +53,24 @@ struct RowBlock {
 
     Frag q[NQ][NK];
     f32x4 acc[NQ][ND];
-    float m[NQ], l[NQ];                                         // l: this lane's keys only
+    // Weights are 2^(y - ref).  ref is the largest logit so far up to kSlack: it is moved up
+    // only when a logit exceeds it by more (thr: by which a logit may; before the first
+    // key every logit moves it), so that the sums are rarely scaled and the lanes of a query
+    // need not agree on a maximum for every key.
+    float ref[NQ], thr[NQ];
+    float l[NQ];                                                // of this lane's keys only
 
     __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int qt = 0; qt < NQ; ++qt) {
-            m[qt] = -INFINITY;
+            ref[qt] = 0.f;
+            thr[qt] = -INFINITY;
             l[qt] = 0.f;
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt) acc[qt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
     }
+    __device__ __forceinline__ float max_logit(int qt) const { return thr[qt] > 0.f ? ref[qt] : -INFINITY; }
     __device__ __forceinline__ void load_q(int qt, const T* row, int g) {
 #pragma unroll
         for (int s = 0; s < NK; ++s)
@@ -90,29 +98,32 @@ struct RowBlock {
             }
         }
     }
-    // y (log2 units, -inf: left out) -> weights, the running maximum moved up first
-    __device__ __forceinline__ void weights(int qt, float (&y)[8]) {
-        float mx = y[0];
+    // y - ref (log2 units, -inf: left out) -> weights; true if ref[qt] moved
+    __device__ __forceinline__ bool weights(int qt, float (&y)[8]) {
+        float mx = fmaxf(y[0], y[1]);
 #pragma unroll
-        for (int j = 1; j < 8; ++j) mx = fmaxf(mx, y[j]);
-        mx = fmaxf(mx, __shfl_xor(mx, 16));
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const float mnew = fmaxf(m[qt], mx);
-        const float ref = mnew == -INFINITY ? 0.f : mnew;       // (no key yet)
-        if (__any(mnew > m[qt])) {
-            const float alpha = fast_exp2(m[qt] - ref);
-            l[qt] *= alpha;
+        for (int j = 2; j < 8; j += 2) mx = fmaxf(fmaxf(mx, y[j]), y[j + 1]);
+        const bool move = __any(mx > thr[qt]);
+        if (move) {
+            mx = fmaxf(mx, __shfl_xor(mx, 16));
+            mx = fmaxf(mx, __shfl_xor(mx, 32));
+            if (mx > thr[qt]) {
+                const float alpha = thr[qt] > 0.f ? fast_exp2(-mx) : 0.f;
+                ref[qt] += mx;
+                thr[qt] = kSlack;
+                l[qt] *= alpha;
 #pragma unroll
-            for (int dt = 0; dt < ND; ++dt) acc[qt][dt] *= alpha;
-            m[qt] = mnew;
+                for (int dt = 0; dt < ND; ++dt) acc[qt][dt] *= alpha;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] -= mx;
+            }
         }
-        float t = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            y[j] = fast_exp2(y[j] - ref);
-            t += y[j];
+            y[j] = fast_exp2(y[j]);
+            l[qt] += y[j];
         }
-        l[qt] += t;
+        return move;
     }
     // acc += V^T P^T; v(dt, j): bf16 the lane's eight keys of column 16 dt + r (j unused),
     // float the key of element j
@@ -150,29 +161,36 @@ __device__ __forceinline__ float over_groups(float v) {
     return v;
 }
 
-// acc[dt] += p V over the keys of `bad` that the query attends to, for the values that are
-// not finite (see the callers: they are zero in the products).  Rare, and slow.
+// Marks, for the values that are not finite in the keys of `bad` (a bit each) that the query
+// at position pos attends to, the feature of the query's row: an infinity of either sign, NaN
+// both.  The four lanes of a query share the keys; v0 is the page's first value row.  Rare.
 template <typename T, int D>
-__device__ __forceinline__ void add_bad(unsigned bad, const T* v0, const float (&p)[8], unsigned seen,
-                                        f32x4 (&acc)[D / 16], int lane) {
+__device__ __forceinline__ void mark_bad(unsigned long long bad, const T* v0, int first, int pos, int lane,
+                                         unsigned (&inf)[2][D / 32]) {
     while (bad) {
-        const int key = __builtin_ctz(bad);
+        const int key = __builtin_ctzll(bad);
         bad &= bad - 1;
-        const int gg = is_bf16<T>() ? key >> 3 : (key & 15) >> 2;
-        const int e = is_bf16<T>() ? key & 7 : 4 * (key >> 4) + (key & 3);
-        float w = p[0];
-#pragma unroll
-        for (int j = 1; j < 8; ++j) w = e == j ? p[j] : w;
-        w = __shfl(w, 16 * gg + (lane & 15));
-        const bool on = (__shfl((int)seen, 16 * gg + (lane & 15)) >> e) & 1;
-#pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt)
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const float x = to_f32(v0[(int64_t)key * D + 16 * dt + 4 * (lane >> 4) + t]);
-                if (on && !__builtin_isfinite(x)) acc[dt][t] += w * x;
-            }
+        if ((key & 3) != lane >> 4 || first + key > pos) continue;
+#pragma unroll 1
+        for (int f = 0; f < D; ++f) {
+            const float x = to_f32(v0[key * D + f]);
+            if (__builtin_isfinite(x)) continue;
+            if (!(x < 0.f)) atomicOr(&inf[0][f >> 5], 1u << (f & 31));
+            if (!(x > 0.f)) atomicOr(&inf[1][f >> 5], 1u << (f & 31));
+        }
     }
+}
+// The marks of a query's row into its sums
+template <int D>
+__device__ __forceinline__ void add_marks(f32x4 (&acc)[D / 16], const unsigned (&inf)[2][D / 32], int g) {
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int f = 16 * dt + 4 * g + t;
+            if (inf[0][f >> 5] >> (f & 31) & 1) acc[dt][t] += INFINITY;
+            if (inf[1][f >> 5] >> (f & 31) & 1) acc[dt][t] -= INFINITY;
+        }
 }
 
 // The sequence and the tile of `rows` tokens in it that global tile number `tile` is, among
@@ -281,7 +299,7 @@ struct PageDma {
 };
 
 // Values that are not finite are kept out of the products, where 0 times them is not 0, and
-// added by add_bad() to the rows that attend to their key.
+// brought into the rows that attend to their key by marks (mark_bad).
 //
 // The values of a tile of which some row leaves something out: rows from `valid` on (never
 // written) become 0, and so does every value that is not finite; bit r of `bad` is set
@@ -318,6 +336,17 @@ __device__ __forceinline__ void clean_values(unsigned char* tile, int valid, uns
     }
 }
 
+// Workgroup -> (head, item).  Workgroups go to the 8 XCDs in turn; each XCD takes every
+// eighth item of every head, heads fastest.  Heads keep different numbers of pages, and
+// this gives each XCD the same share of each; the workgroups at work on an XCD at one time
+// are neighbouring items of all heads, so that those that read the same pages share its L2.
+__device__ __forceinline__ void deal(int heads, int& h, int& item) {
+    const int x = blockIdx.x & 7, k = blockIdx.x >> 3;
+    h = k % heads;
+    item = k / heads * 8 + x;
+}
+__host__ inline unsigned dealt(int64_t items, int heads) { return (unsigned)((items + 7) / 8 * 8 * heads); }
+
 // Row t, head h of the output, or its share of the part `sp` of `splits`
 template <typename T, int D>
 __device__ __forceinline__ void put_row(const PagedArgs& a, int t, int h, int sp, int splits, int stride,
@@ -345,13 +374,16 @@ __device__ __forceinline__ void put_row(const PagedArgs& a, int t, int h, int sp
 }
 
 // ---- long ------------------------------------------------------------------------------
-template <typename T, int D>
+template <typename T, int D, int NQ>
 struct alignas(1024) LongSmem {
     unsigned char k[2][64 * D * sizeof(T)];
     unsigned char v[2][64 * D * sizeof(T)];
-    double c[2][64];         // cumulative gates of the page
-    float kb[2][64];         // (R - c_j) log2(e)
-    unsigned bad[2][2];
+    float kb[2][64];         // (c_j - R) log2(e), negated
+    float2 kd[2][64];        // c_j - R as a sum of two floats
+    double end[2];           // c of the page's last position
+    unsigned bad[2][2];      // keys of the page with values that are not finite
+    unsigned inf[64 * NQ][2][D / 32];
+    int marked;
 };
 
 template <typename T, int D, int NQ>
@@ -359,12 +391,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 && 
 void paged_long_kernel(PagedArgs a, int tiles, int splits, int stride, int short_max, float kscale) {
     constexpr int kRows = 64 * NQ;
     typedef RowBlock<T, D, NQ> Block;
-    __shared__ LongSmem<T, D> sm;
+    __shared__ LongSmem<T, D, NQ> sm;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int lane = threadIdx.x & 63, g = lane >> 4, r16 = lane & 15;
-    // heads fastest: they keep different numbers of pages, and this spreads each over the XCDs
-    const int h = blockIdx.x % a.H, rest = blockIdx.x / a.H;
+    int h, rest;
+    deal(a.H, h, rest);
     const int sp = rest % splits;
+    if (rest / splits >= tiles) return;
     int s, tile;
     // (the last tiles of a sequence have the most pages: they go first)
     if (!locate(a, tiles - 1 - rest / splits, kRows, short_max, 0x7fffffff, lane, s, tile)) return;
@@ -382,27 +415,36 @@ void paged_long_kernel(PagedArgs a, int tiles, int splits, int stride, int short
     };
     const double R = gate(p0);
     const int lo = first_page(a, s, h, p0 >> 6, R, delta, lane);
-    const int pages = nd1 - lo + 1, per = (pages + splits - 1) / splits;
-    const int nb = lo + sp * per, ne = min(nb + per - 1, nd1);       // this part's pages
+    // this part's pages, of those the table has (the last one there may be is W - 1)
+    const int top = min(nd1, a.W - 1), pages = max(top - lo + 1, 0), per = (pages + splits - 1) / splits;
+    const int nb = lo + sp * per, ne = min(nb + per - 1, top);
+    if (nd1 >= a.W && wave == 0) report(a, s, h, lane);
 
     Block blk;
     blk.clear();
     // rows of the wave and of the lane (those past the end repeat the last one)
-    const int w0 = p0 + 16 * NQ * wave, w1 = min(w0 + 16 * NQ - 1, p1);
-    const bool wave_on = w0 <= p1;
+    // (counted from p0: positions may be as large as an int holds)
+    const int o0 = 16 * NQ * wave;
+    const bool wave_on = o0 < rows;
+    const int w0 = p0 + min(o0, rows - 1), w1 = p0 + min(o0 + 16 * NQ - 1, rows - 1);
     double ci[NQ];
     int pi[NQ];
-    float init[NQ], zero[NQ];
-    const float sqrt_d = sqrtf((float)D);
+    float2 rd[NQ];                                                   // c_i - R likewise
+    float row[NQ], init[NQ], zero[NQ];                               // row term and start of the scores
+    const float per_y = sqrtf((float)D) * kLn2;                      // q.k per unit of y
 #pragma unroll
     for (int qt = 0; qt < NQ; ++qt) {
-        pi[qt] = min(w0 + 16 * qt + r16, p1);
+        pi[qt] = p0 + min(o0 + 16 * qt + r16, rows - 1);
         ci[qt] = gate(pi[qt]);
         blk.load_q(qt, (const T*)a.q + (int64_t)(q.row0 + pi[qt] - q.past) * a.qt + (int64_t)h * a.qh, g);
-        init[qt] = (float)(ci[qt] - R) * sqrt_d;
+        const double r = ci[qt] - R;
+        rd[qt].x = (float)r;
+        rd[qt].y = (float)(r - (double)rd[qt].x);
+        row[qt] = rd[qt].x * kLog2e;
+        init[qt] = row[qt] * per_y;
         zero[qt] = 0.f;
     }
-    const double c_first = readfirst_f64(ci[0]), c_last = wave_on ? gate(w1) : 0.0;
+    const double c_first = readfirst_f64(ci[0]);
     const double c_tile_last = gate(p1);
 
     PageDma<T, D> dma;
@@ -422,8 +464,11 @@ void paged_long_kernel(PagedArgs a, int tiles, int splits, int stride, int short
     };
     auto put_gates = [&](int buf) __attribute__((always_inline)) {
         if (threadIdx.x < 64) {
-            sm.c[buf][threadIdx.x] = cn;
-            sm.kb[buf][threadIdx.x] = (float)(R - cn) * kLog2e;
+            const double r = cn - R;
+            const float hi = (float)r;
+            sm.kb[buf][threadIdx.x] = -hi * kLog2e;
+            sm.kd[buf][threadIdx.x] = make_float2(hi, (float)(r - (double)hi));
+            if (threadIdx.x == 63) sm.end[buf] = cn;
             if (threadIdx.x < 2) sm.bad[buf][threadIdx.x] = 0;
         }
     };
@@ -434,11 +479,16 @@ void paged_long_kernel(PagedArgs a, int tiles, int splits, int stride, int short
     for (int p = 0; p < Block::NK; ++p)
         koff[p] = is_bf16<T>() ? tile_off(key_row<T>(0, r16), 32 * p + 8 * g) : f32_off<D>(r16, 16 * p + 4 * g);
 
-    auto step = [&](auto mask_tag, int n, int buf, int page, unsigned long long bad) __attribute__((always_inline)) {
+    int voff[is_bf16<T>() ? Block::ND : 1];
+    if constexpr (is_bf16<T>())
+#pragma unroll
+        for (int dt = 0; dt < Block::ND; ++dt) voff[dt] = tile_off(8 * g + (r16 >> 2), 16 * dt + 4 * (r16 & 3));
+
+    auto step = [&](auto mask_tag, int n, int buf) __attribute__((always_inline)) {
         constexpr bool kMask = decltype(mask_tag)::value;
         bool keep[NQ];
         if constexpr (kMask) {
-            const double end = sm.c[buf][63];
+            const double end = sm.end[buf];
 #pragma unroll
             for (int qt = 0; qt < NQ; ++qt) keep[qt] = n >= (pi[qt] >> 6) || ci[qt] - end >= delta;
         }
@@ -454,84 +504,91 @@ void paged_long_kernel(PagedArgs a, int tiles, int splits, int stride, int short
             });
             __builtin_amdgcn_sched_barrier(0);
             float p[NQ][8];
-            unsigned seen[NQ];
 #pragma unroll
             for (int qt = 0; qt < NQ; ++qt) {
-                seen[qt] = kMask ? 0 : 0xff;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const int key = 32 * ks + key_of<T>(g, j);
                     float y;
                     if constexpr (kMask) {
+                        const float2 kd = sm.kd[buf][key];
+                        const float decay = (rd[qt].x - kd.x) + (rd[qt].y - kd.y);
                         y = __builtin_fmaf(x[j >> 2][qt][j & 3], kscale,
-                                           (float)(ci[qt] - sm.c[buf][key]) * kLog2e);
-                        const bool on = keep[qt] && 64 * n + key <= pi[qt];
-                        seen[qt] |= (unsigned)on << j;
-                        if (!on) y = -INFINITY;
+                                           __builtin_fmaf(decay, kLog2e, -blk.ref[qt]));
+                        if (!keep[qt] || 64 * n + key > pi[qt]) y = -INFINITY;
                     } else {
                         y = __builtin_fmaf(x[j >> 2][qt][j & 3], kscale, sm.kb[buf][key]);
                     }
                     p[qt][j] = y;
                 }
-                blk.weights(qt, p[qt]);
+                if (blk.weights(qt, p[qt])) init[qt] = (row[qt] - blk.ref[qt]) * per_y;
             }
             __builtin_amdgcn_sched_barrier(0);
             blk.add(p, [&](int dt, int j) __attribute__((always_inline)) {
                 if constexpr (is_bf16<T>())
-                    return tile_col8(sm.v[buf], 32 * ks + 8 * g, 16 * dt, r16);
+                    return tile_col8_at(sm.v[buf] + voff[dt] + 128 * 32 * ks);
                 else
                     return *reinterpret_cast<const float*>(
                         sm.v[buf] + f32_off<D>(32 * ks + key_of<T>(g, j), 16 * dt + r16));
             });
-            {
-                const unsigned b = (unsigned)(bad >> (32 * ks));
-                if (b) {
-                    const T* v0 = vp + (((int64_t)page * a.Hk + hk) * 64 + 32 * ks) * D;
-#pragma unroll
-                    for (int qt = 0; qt < NQ; ++qt)
-                        add_bad<T, D>(b, v0, p[qt], seen[qt], blk.acc[qt], lane);
-                }
-            }
         }
         __builtin_amdgcn_sched_barrier(0);
     };
 
+    if (threadIdx.x == 0) sm.marked = 0;
+    for (int i = threadIdx.x; i < 64 * NQ * 2 * (D / 32); i += 256) (&sm.inf[0][0][0])[i] = 0;
     if (nb <= ne) {
         win.fill(a, s, nb, lane);
         issue(nb, 0);
         put_gates(0);
         wait_vmcnt0();
         __syncthreads();
-        int buf = 0;
-        for (int n = nb; n <= ne; ++n, buf ^= 1) {
+        int buf = 0, n = nb;
+        // some row of the tile leaves out something of page n (in buffer buf)
+        auto partly = [&]() { return n >= (p0 >> 6) || !(c_tile_last - sm.end[buf] >= delta); };
+        auto next = [&](auto mask_tag) __attribute__((always_inline)) {
+            constexpr bool kMask = decltype(mask_tag)::value;
             const int page = page_next;
-            const bool ok = page >= 0;
             if (n < ne) issue(n + 1, buf ^ 1);
-            const double end = sm.c[buf][63];
-            // some row of the tile leaves out something of this page
-            const bool partly = n >= (p0 >> 6) || !(c_tile_last - end >= delta);
             unsigned long long bad = 0;
-            if (ok && partly) {
+            if (kMask && page >= 0) {
                 clean_values<T, D>(sm.v[buf], len - 64 * n, sm.bad[buf], threadIdx.x, 256);
                 lds_barrier();
                 bad = (unsigned long long)sm.bad[buf][1] << 32 | sm.bad[buf][0];
             }
-            if (ok && wave_on && n <= (w1 >> 6) && (n >= (w0 >> 6) || c_first - end >= delta)) {
-                if (n < (w0 >> 6) && c_last - end >= delta) step(std::false_type{}, n, buf, page, bad);
-                else step(std::true_type{}, n, buf, page, bad);
+            if (page >= 0 && wave_on &&
+                (!kMask || (n <= (w1 >> 6) && (n >= (w0 >> 6) || c_first - sm.end[buf] >= delta))))
+                step(mask_tag, n, buf);
+            if (kMask && bad && wave_on) {
+                sm.marked = 1;
+#pragma unroll 1
+                for (int qt = 0; qt < NQ; ++qt) {
+                    const int pos = p0 + min(o0 + 16 * qt + r16, rows - 1);
+                    if (o0 + 16 * qt + r16 < rows && (n >= (pos >> 6) || gate(pos) - sm.end[buf] >= delta))
+                        mark_bad<T, D>(bad, vp + ((int64_t)page * a.Hk + hk) * 64 * D, 64 * n, pos, lane,
+                                       sm.inf[16 * (NQ * wave + qt) + r16]);
+                }
             }
-            if (!ok && wave == 0) report(a, s, h, lane);
+            if (page < 0 && wave == 0) report(a, s, h, lane);
             if (n < ne) put_gates(buf ^ 1);
             wait_vmcnt0_lgkmcnt0();
             __syncthreads();
+            ++n;
+            buf ^= 1;
+        };
+        // (two loops: one with both forms of the step needs more registers than there are)
+        while (n <= ne) {
+            while (n <= ne && !partly()) next(std::false_type{});
+            while (n <= ne && partly()) next(std::true_type{});
         }
     }
     if (!wave_on) return;
 #pragma unroll
     for (int qt = 0; qt < NQ; ++qt) {
         const float l = over_groups(blk.l[qt]);
-        if (w0 + 16 * qt + r16 > p1) continue;
-        put_row<T, D>(a, q.row0 + pi[qt] - q.past, h, sp, splits, stride, blk.acc[qt], blk.m[qt], l, g);
+        if (o0 + 16 * qt + r16 >= rows) continue;
+        if (nb <= ne && sm.marked) add_marks<D>(blk.acc[qt], sm.inf[16 * (NQ * wave + qt) + r16], g);
+        put_row<T, D>(a, q.row0 + pi[qt] - q.past, h, sp, splits, stride, blk.acc[qt], blk.max_logit(qt), l, g);
     }
 }
 
@@ -541,6 +598,8 @@ struct alignas(1024) ShortSmem {
     // value tiles of each wave (bf16; float values go straight to registers)
     unsigned char v[4][2][is_bf16<T>() ? 64 * D * 2 : 1024];
     unsigned bad[4][2];
+    unsigned inf[16][2][D / 32];
+    int marked;
     float m[4][16], l[4][16];
     int first[16];
 };
@@ -555,7 +614,8 @@ __global__ __launch_bounds__(256) void paged_short_kernel(PagedArgs a, int split
     __shared__ ShortSmem<T, D> sm;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int lane = threadIdx.x & 63, g = lane >> 4, r16 = lane & 15;
-    const int hk = blockIdx.x % a.Hk, rest = blockIdx.x / a.Hk;
+    int hk, rest;
+    deal(a.Hk, hk, rest);
     const int sp = rest % splits;
     int s, tile;
     if (!locate(a, rest / splits, short_max, 0, short_max, lane, s, tile)) return;
@@ -578,12 +638,14 @@ __global__ __launch_bounds__(256) void paged_short_kernel(PagedArgs a, int split
         const int f = first_page(a, s, hk * G + k, q.past >> 6, ck, dk, lane);
         if (lane == 0) sm.first[k] = f;
     }
-    if (lane < 2) sm.bad[wave][lane] = 0;
+    if (threadIdx.x == 0) sm.marked = 0;
+    for (int i = threadIdx.x; i < 16 * 2 * (D / 32); i += 256) (&sm.inf[0][0][0])[i] = 0;
     __syncthreads();
     int lo = sm.first[0];
     for (int k = 1; k < G; ++k) lo = min(lo, sm.first[k]);
-    const int pages = nd1 - lo + 1, per = (pages + splits - 1) / splits;
-    const int nb = lo + sp * per, ne = min(nb + per - 1, nd1);
+    const int top = min(nd1, a.W - 1), pages = max(top - lo + 1, 0), per = (pages + splits - 1) / splits;
+    const int nb = lo + sp * per, ne = min(nb + per - 1, top);
+    if (nd1 >= a.W && r16 < nrows) report(a, s, h, lane & 48);
 
     const T* kp = (const T*)a.kp;
     const T* vp = (const T*)a.vp;
@@ -687,7 +749,7 @@ __global__ __launch_bounds__(256) void paged_short_kernel(PagedArgs a, int split
                     const unsigned long long b = __ballot(found);
 #pragma unroll
                     for (int gg = 0; gg < 4; ++gg)
-                        if ((b >> (16 * gg)) & 0xffffull) bad |= 1ull << key_of<T>(gg, j);
+                        if ((b >> (16 * gg)) & 0xffffull) bad |= 1ull << (32 * hf + key_of<T>(gg, j));
                 }
             }
         }
@@ -697,13 +759,12 @@ __global__ __launch_bounds__(256) void paged_short_kernel(PagedArgs a, int split
             const float zero[1] = {0.f};
             blk.scores(x, zero, [&](int kk, int i) __attribute__((always_inline)) { return kc[ks][kk][i]; });
             float p[1][8];
-            unsigned seen = 0;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int key = 32 * (ks + hf) + key_of<T>(g, j);
                 const bool on = keep && 64 * n + key <= pi;
-                seen |= (unsigned)on << j;
-                const float y = __builtin_fmaf(x[j >> 2][0][j & 3], kscale, (float)(ci - cc[ks][j]) * kLog2e);
+                const float y = __builtin_fmaf(x[j >> 2][0][j & 3], kscale,
+                                               __builtin_fmaf((float)(ci - cc[ks][j]), kLog2e, -blk.ref[0]));
                 p[0][j] = on ? y : -INFINITY;
             }
             blk.weights(0, p[0]);
@@ -711,17 +772,18 @@ __global__ __launch_bounds__(256) void paged_short_kernel(PagedArgs a, int split
                 if constexpr (is_bf16<T>()) return tile_col8(sm.v[wave][buf], 32 * ks + 8 * g, 16 * dt, r16);
                 else return vc[dt][j];
             });
-            const unsigned b = (unsigned)(bad >> (32 * ks));
-            if (b)
-                add_bad<T, D>(b, vp + (((int64_t)pg * a.Hk + hk) * 64 + 32 * (ks + hf)) * D, p[0], seen,
-                              blk.acc[0], lane);
+        }
+        if (bad) {
+            sm.marked = 1;
+            if (keep && r16 < nrows)
+                mark_bad<T, D>(bad, vp + ((int64_t)pg * a.Hk + hk) * 64 * D, 64 * n, pi, lane, sm.inf[r16]);
         }
     }
 
     // the four waves' sums: maxima and sums first, then O through the value tiles' LDS
     const float l = over_groups(blk.l[0]);
     if (g == 0) {
-        sm.m[wave][r16] = blk.m[0];
+        sm.m[wave][r16] = blk.max_logit(0);
         sm.l[wave][r16] = l;
     }
     __syncthreads();
@@ -731,7 +793,7 @@ __global__ __launch_bounds__(256) void paged_short_kernel(PagedArgs a, int split
     const float ref = M == -INFINITY ? 0.f : M;
 #pragma unroll
     for (int w = 0; w < 4; ++w) L += sm.l[w][r16] * fast_exp2(sm.m[w][r16] - ref);
-    const float scale = fast_exp2(blk.m[0] - ref);
+    const float scale = fast_exp2(blk.max_logit(0) - ref);
     // [wave][dt][lane]; the first three waves' tiles are no longer read
     __shared__ f32x4 o_s[3][ND][64];
     if (wave > 0)
@@ -746,6 +808,7 @@ __global__ __launch_bounds__(256) void paged_short_kernel(PagedArgs a, int split
         for (int w = 0; w < 3; ++w) o += o_s[w][dt][lane];
         blk.acc[0][dt] = o;
     }
+    if (sm.marked) add_marks<D>(blk.acc[0], sm.inf[r16], g);
     if (r16 < nrows) put_row<T, D>(a, q.row0 + r / G, h, sp, splits, stride, blk.acc[0], M, L, g);
 }
 
@@ -786,7 +849,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a, int split_
     float o0 = 0.f, o1 = 0.f;
     for (int p = 0; p < splits; ++p) {
         const float wp = __shfl(w, p);
-        if (wp == 0.f) continue;                        // (its sums may not be there)
+        if (__shfl(v.y, p) == 0.f) continue;            // (no key: its sums are not there)
         o0 = __builtin_fmaf(wp, po[(int64_t)p * D + lane], o0);
         if (D == 128) o1 = __builtin_fmaf(wp, po[(int64_t)p * D + 64 + lane], o1);
     }
@@ -850,7 +913,7 @@ template <typename T, int D>
 void attend(const PagedArgs& a, const Division& v, hipStream_t s) {
     const float kscale = kLog2e / sqrtf((float)D);
     if (v.long_on) {
-        const dim3 grid((unsigned)((int64_t)v.tiles_long * v.split_long * a.H));
+        const dim3 grid(dealt((int64_t)v.tiles_long * v.split_long, a.H));
         const int sm = v.short_on ? v.short_max : 0;
         if (v.nq == 2)
             hipLaunchKernelGGL((paged_long_kernel<T, D, 2>), grid, dim3(256), 0, s, a, v.tiles_long,
@@ -861,8 +924,8 @@ void attend(const PagedArgs& a, const Division& v, hipStream_t s) {
     }
     if (v.short_on)
         hipLaunchKernelGGL((paged_short_kernel<T, D>),
-                           dim3((unsigned)((int64_t)v.tiles_short * v.split_short * a.Hk)), dim3(256), 0, s, a,
-                           v.split_short, v.stride, v.short_max, kscale);
+                           dim3(dealt((int64_t)v.tiles_short * v.split_short, a.Hk)), dim3(256), 0,
+                           s, a, v.split_short, v.stride, v.short_max, kscale);
     if (v.stride > 1)
         hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3((unsigned)(((int64_t)a.T * a.H + 3) / 4)), dim3(256),
                            0, s, a, v.split_long, v.split_short, v.stride, v.short_on ? v.short_max : 0,

@@ -360,7 +360,8 @@ def test_corrupt_call_arrays_stay_inside():
             w.past_t = torch.tensor(past, dtype=torch.int32, device="cuda")
             q = torch.zeros((75, 2, 64), dtype=BF, device="cuda")
             w.cache.append(q, q, torch.zeros((75, 2), device="cuda"), w.cu, w.past_t, w.table)
-            w.cache.attend(q, w.cu, w.past_t, w.table, 75, gamma_q=w.gq, gamma_k=w.gk, eps=EPS)
+            for eps in (EPS, 0.0):
+                w.cache.attend(q, w.cu, w.past_t, w.table, 75, gamma_q=w.gq, gamma_k=w.gk, eps=eps)
     torch.cuda.synchronize()
 
 
