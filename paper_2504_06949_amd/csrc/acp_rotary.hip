@@ -6,6 +6,8 @@
 // angles depend on the position alone.  Angles are p f_i in turns, reduced to [-1/2, 1/2]
 // in float64 (exact to 2^-53 of the angle), so that sine and cosine are those of the true
 // angle at any position below 2^31.
+#include <type_traits>
+
 #include "acp_device.h"
 #include "acp_ops_internal.h"
 
@@ -19,24 +21,26 @@ struct RotaryKernelArgs {
     int split;               // threads that share the heads of a position's chunk
 };
 
-template <typename T, int VEC>
+// VEC features from p, aligned to the element only (gfx950 moves them in one instruction all
+// the same).  FULL: all are inside the row, else the first `left`.
+template <bool FULL, typename T, int VEC>
 __device__ __forceinline__ void get(const T* p, int left, T (&v)[VEC]) {
-    if (left >= VEC) __builtin_memcpy(v, p, sizeof(v));
+    if (FULL || left >= VEC) __builtin_memcpy(v, p, sizeof(v));
     else
 #pragma unroll
         for (int i = 0; i < VEC; ++i)
             if (i < left) v[i] = p[i];
 }
-template <typename T, int VEC>
+template <bool FULL, typename T, int VEC>
 __device__ __forceinline__ void put(T* p, int left, const T (&v)[VEC]) {
-    if (left >= VEC) __builtin_memcpy(p, v, sizeof(v));
+    if (FULL || left >= VEC) __builtin_memcpy(p, v, sizeof(v));
     else
 #pragma unroll
         for (int i = 0; i < VEC; ++i)
             if (i < left) p[i] = v[i];
 }
 
-template <typename T, bool INTER>
+template <typename T, bool INTER, bool FULL>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryKernelArgs ka, int64_t items) {
     constexpr int C = 16 / (int)sizeof(T);      // pairs per chunk
     const RotaryArgs& a = ka.a;
@@ -50,68 +54,85 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryKernelArgs ka, int64_
     const int h0 = (int)((int64_t)both * blockIdx.y / ka.split);
     const int h1 = (int)((int64_t)both * (blockIdx.y + 1) / ka.split);
 
-    auto src = [&](int h) {
-        const int w = h >= a.heads[0];
-        const Strides& s = a.xs[w];
-        return (const T*)a.x[w] + b * s.b + (int64_t)(h - (w ? a.heads[0] : 0)) * s.h + l * s.l;
+    // the thread's position in each tensor; head h of the two together
+    const T* xb[2];
+    T* yb[2];
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        xb[w] = (const T*)a.x[w] + b * a.xs[w].b + l * a.xs[w].l;
+        yb[w] = (T*)a.y[w] + b * a.ys[w].b + l * a.ys[w].l;
+    }
+    auto src = [&](int h) __attribute__((always_inline)) {
+        return h < a.heads[0] ? xb[0] + h * a.xs[0].h : xb[1] + (h - a.heads[0]) * a.xs[1].h;
     };
-    auto dst = [&](int h) {
-        const int w = h >= a.heads[0];
-        const Strides& s = a.ys[w];
-        return (T*)a.y[w] + b * s.b + (int64_t)(h - (w ? a.heads[0] : 0)) * s.h + l * s.l;
+    auto dst = [&](int h) __attribute__((always_inline)) {
+        return h < a.heads[0] ? yb[0] + h * a.ys[0].h : yb[1] + (h - a.heads[0]) * a.ys[1].h;
     };
 
-    if (ch >= ka.chunks) {
-        const int e = a.rot + (ch - ka.chunks) * 2 * C, left = a.d - e;
-        for (int h = h0; h < h1; ++h) {
-            T v[2 * C];
-            get<T, 2 * C>(src(h) + e, left, v);
-            put<T, 2 * C>(dst(h) + e, left, v);
-        }
-        return;
-    }
     int64_t p = a.start + l;
     if (a.pos) {
         const int64_t o = b * a.pos_b + l * a.pos_l;
         p = a.pos_bytes == 4 ? ((const int*)a.pos)[o] : ((const int64_t*)a.pos)[o];
     }
-    const int half = a.rot / 2, i0 = ch * C, left = half - i0;
+    // The chunk's two vectors of C features: of a chunk of pairs or of one that is copied.
+    // FULL: the last chunk of either kind may start earlier and repeat part of the one before
+    const int half = a.rot / 2;
+    const bool copy = ch >= ka.chunks;
+    int i0 = ch * C, e = a.rot + (ch - ka.chunks) * 2 * C;
+    if (FULL) {
+        i0 = min(i0, half - C);
+        e = min(e, a.d - 2 * C);
+    }
+    const int off = copy ? e : INTER ? 2 * i0 : i0, far = copy || INTER ? C : half;
+    const int left_a = copy ? a.d - e : INTER ? a.rot - 2 * i0 : half - i0;
+    const int left_b = copy || INTER ? left_a - C : left_a;
     float cs[C], sn[C];
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-        const double t = (double)p * a.turns[min(i0 + i, half - 1)];
+        const double t = (double)p * a.turns[min(max(i0 + i, 0), half - 1)];
         float s, c;
         sincospif(2.0f * (float)(t - rint(t)), &s, &c);
         cs[i] = c * a.amplitude;
         sn[i] = (a.inverse ? -s : s) * a.amplitude;
     }
-    for (int h = h0; h < h1; ++h) {
-        const T* x = src(h);
-        T* y = dst(h);
-        if constexpr (INTER) {
-            T v[2 * C];
-            get<T, 2 * C>(x + 2 * i0, 2 * left, v);
+    // Several heads at a time, all loads before the first store (which could be of the same
+    // memory, for all the compiler knows)
+    auto group = [&](auto count, int hb) __attribute__((always_inline)) {
+        constexpr int N = decltype(count)::value;
+        T v[N][C], z[N][C];
 #pragma unroll
-            for (int i = 0; i < C; ++i) {
-                const float u = to_f32(v[2 * i]), w = to_f32(v[2 * i + 1]);
-                v[2 * i] = from_f32<T>(u * cs[i] - w * sn[i]);
-                v[2 * i + 1] = from_f32<T>(u * sn[i] + w * cs[i]);
-            }
-            put<T, 2 * C>(y + 2 * i0, 2 * left, v);
-        } else {
-            T v[C], z[C];
-            get<T, C>(x + i0, left, v);
-            get<T, C>(x + half + i0, left, z);
-#pragma unroll
-            for (int i = 0; i < C; ++i) {
-                const float u = to_f32(v[i]), w = to_f32(z[i]);
-                v[i] = from_f32<T>(u * cs[i] - w * sn[i]);
-                z[i] = from_f32<T>(u * sn[i] + w * cs[i]);
-            }
-            put<T, C>(y + i0, left, v);
-            put<T, C>(y + half + i0, left, z);
+        for (int k = 0; k < N; ++k) {
+            const T* x = src(hb + k) + off;
+            get<FULL>(x, left_a, v[k]);
+            get<FULL>(x + far, left_b, z[k]);
         }
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            T o[2 * C];
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+                // pair i: interleaved, features 2 i and 2 i + 1 of the 2 C in v and z
+                const float u = to_f32(!INTER ? v[k][i] : 2 * i < C ? v[k][2 * i % C] : z[k][2 * i % C]);
+                const float w = to_f32(!INTER ? z[k][i] : 2 * i < C ? v[k][(2 * i + 1) % C] : z[k][(2 * i + 1) % C]);
+                o[INTER ? 2 * i : i] = from_f32<T>(u * cs[i] - w * sn[i]);
+                o[INTER ? 2 * i + 1 : C + i] = from_f32<T>(u * sn[i] + w * cs[i]);
+            }
+            if (!copy) {
+                __builtin_memcpy(v[k], o, sizeof(v[k]));
+                __builtin_memcpy(z[k], o + C, sizeof(z[k]));
+            }
+            T* y = dst(hb + k) + off;
+            put<FULL>(y, left_a, v[k]);
+            put<FULL>(y + far, left_b, z[k]);
+        }
+    };
+    int h = h0;
+    for (; h + 4 <= h1; h += 4) group(std::integral_constant<int, 4>{}, h);
+    if (h + 2 <= h1) {
+        group(std::integral_constant<int, 2>{}, h);
+        h += 2;
     }
+    if (h < h1) group(std::integral_constant<int, 1>{}, h);
 }
 
 template <typename T>
@@ -120,9 +141,11 @@ void rotary(const RotaryArgs& a, hipStream_t s) {
     RotaryKernelArgs k{a, 0, 0, 1};
     k.chunks = (a.rot / 2 + C - 1) / C;
     // (a tensor turned in place needs no copy of the rest; both must be)
-    bool in_place = true;
-    for (int w = 0; w < 2; ++w)
+    bool in_place = true, apart = true;
+    for (int w = 0; w < 2; ++w) {
         if (a.x[w] && a.x[w] != a.y[w]) in_place = false;
+        if (a.x[w] && a.x[w] == a.y[w]) apart = false;
+    }
     k.copies = in_place ? 0 : (a.d - a.rot + 2 * C - 1) / (2 * C);
     const int64_t items = (int64_t)a.B * a.L * (k.chunks + k.copies);
     const int both = a.heads[0] + a.heads[1];
@@ -130,8 +153,17 @@ void rotary(const RotaryArgs& a, hipStream_t s) {
     const int64_t want = ((int64_t)256 * 2048 + items - 1) / items;
     k.split = want < both ? (int)want : both;
     const dim3 grid((unsigned)((items + 255) / 256), k.split);
-    if (a.interleaved) hipLaunchKernelGGL((rotary_kernel<T, true>), grid, dim3(256), 0, s, k, items);
-    else hipLaunchKernelGGL((rotary_kernel<T, false>), grid, dim3(256), 0, s, k, items);
+    // Vectors that end with the row's part: where its length is no multiple of them the last
+    // one repeats features of the one before, which two threads then turn alike (not in
+    // place, where the second would turn them again); shorter parts go feature by feature.
+    const auto whole_chunks = [&](int n, int c) { return n % c == 0 || (n >= c && apart); };
+    const bool full = whole_chunks(a.rot / 2, C) && (k.copies == 0 || whole_chunks(a.d - a.rot, 2 * C));
+    auto run = [&](auto inter, auto whole) {
+        hipLaunchKernelGGL((rotary_kernel<T, decltype(inter)::value, decltype(whole)::value>), grid, dim3(256), 0,
+                           s, k, items);
+    };
+    if (a.interleaved) full ? run(std::true_type{}, std::true_type{}) : run(std::true_type{}, std::false_type{});
+    else full ? run(std::false_type{}, std::true_type{}) : run(std::false_type{}, std::false_type{});
 }
 
 }  // namespace

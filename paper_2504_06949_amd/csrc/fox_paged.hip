@@ -403,7 +403,7 @@ void paged_long_kernel(PagedArgs a, int tiles, int splits, int stride, int short
     if (!locate(a, tiles - 1 - rest / splits, kRows, short_max, 0x7fffffff, lane, s, tile)) return;
     const Seq q = seq_of(a, s);
     const int hk = h / (a.H / a.Hk);
-    const double delta = head_delta(a, h);
+    const double delta = readfirst_f64(head_delta(a, h));
     const int row0 = tile * kRows, rows = min(kRows, q.n - row0);    // of the sequence's new rows
     const int p0 = q.past + row0, p1 = p0 + rows - 1;                // positions of the tile
     const int len = q.past + q.n;
@@ -413,7 +413,7 @@ void paged_long_kernel(PagedArgs a, int tiles, int splits, int stride, int short
         const int p = page_of(a, s, pos >> 6);
         return p < 0 ? 0.0 : gates_of(a, p, h)[pos & 63];
     };
-    const double R = gate(p0);
+    const double R = readfirst_f64(gate(p0));
     const int lo = first_page(a, s, h, p0 >> 6, R, delta, lane);
     // this part's pages, of those the table has (the last one there may be is W - 1)
     const int top = min(nd1, a.W - 1), pages = max(top - lo + 1, 0), per = (pages + splits - 1) / splits;
@@ -430,7 +430,7 @@ void paged_long_kernel(PagedArgs a, int tiles, int splits, int stride, int short
     double ci[NQ];
     int pi[NQ];
     float2 rd[NQ];                                                   // c_i - R likewise
-    float row[NQ], init[NQ], zero[NQ];                               // row term and start of the scores
+    float init[NQ], zero[NQ];                                        // start of the scores
     const float per_y = sqrtf((float)D) * kLn2;                      // q.k per unit of y
 #pragma unroll
     for (int qt = 0; qt < NQ; ++qt) {
@@ -440,12 +440,11 @@ void paged_long_kernel(PagedArgs a, int tiles, int splits, int stride, int short
         const double r = ci[qt] - R;
         rd[qt].x = (float)r;
         rd[qt].y = (float)(r - (double)rd[qt].x);
-        row[qt] = rd[qt].x * kLog2e;
-        init[qt] = row[qt] * per_y;
+        init[qt] = rd[qt].x * (kLog2e * per_y);
         zero[qt] = 0.f;
     }
     const double c_first = readfirst_f64(ci[0]);
-    const double c_tile_last = gate(p1);
+    const double c_tile_last = readfirst_f64(gate(p1));
 
     PageDma<T, D> dma;
     dma.init(wave, lane);
@@ -521,7 +520,7 @@ void paged_long_kernel(PagedArgs a, int tiles, int splits, int stride, int short
                     }
                     p[qt][j] = y;
                 }
-                if (blk.weights(qt, p[qt])) init[qt] = (row[qt] - blk.ref[qt]) * per_y;
+                if (blk.weights(qt, p[qt])) init[qt] = __builtin_fmaf(rd[qt].x, kLog2e, -blk.ref[qt]) * per_y;
             }
             __builtin_amdgcn_sched_barrier(0);
             blk.add(p, [&](int dt, int j) __attribute__((always_inline)) {
