@@ -122,11 +122,11 @@ acp::PagedArgs paged_args(acp_dtype dt, int T, int N, int W, int P, int H, int H
     return a;
 }
 
-acp_status check_division(int T, int H, int max_new, int64_t max_len) {
+acp_status check_division(int T, int N, int H, int max_new, int64_t max_len) {
     if (max_new < 0 || max_len < 0 || max_len > ((int64_t)1 << 31))
         return set_error(ACP_EINVAL, "max_new=%d or max_len=%lld outside their range", max_new, (long long)max_len);
-    if ((int64_t)T * H > (int64_t)1 << 28)
-        return set_error(ACP_EUNSUPPORTED, "T*H=%lld exceeds 2^28", (long long)T * H);
+    if ((int64_t)T * H > (int64_t)1 << 28 || (int64_t)N * H > (int64_t)1 << 28)
+        return set_error(ACP_EUNSUPPORTED, "T*H=%lld or N*H=%lld exceeds 2^28", (long long)T * H, (long long)N * H);
     return ACP_OK;
 }
 
@@ -344,9 +344,10 @@ acp_status acp_paged_workspace_size(int T, int N, int H, int Hk, int d, acp_dtyp
                                     int64_t max_len, size_t* bytes) {
     ACP_TRY(check_paged(1, H, Hk, d, dt));
     if (T < 0 || N < 0) return set_error(ACP_EINVAL, "bad sizes (T=%d N=%d)", T, N);
-    ACP_TRY(check_division(T, H, max_new, max_len));
+    ACP_TRY(check_division(T, N, H, max_new, max_len));
     if (bytes == nullptr) return set_error(ACP_EINVAL, "bytes is NULL");
     acp::PagedArgs a{};
+    a.bf16 = dt == ACP_BF16;
     a.T = T; a.N = N; a.H = H; a.Hk = Hk; a.d = d;
     a.max_new = max_new; a.max_len = max_len;
     *bytes = acp::paged_workspace(a);
@@ -361,7 +362,7 @@ acp_status fox_attn_paged(const void* q, const int64_t* q_strides, acp_dtype dt,
     ACP_TRY(check_paged(P, H, Hk, d, dt));
     ACP_TRY(check_call(T, N, W, cu, past, table));
     ACP_TRY(check_cache(cache, cache_bytes, paged_layout(P, H, Hk, d, dt)));
-    ACP_TRY(check_division(T, H, max_new, max_len));
+    ACP_TRY(check_division(T, N, H, max_new, max_len));
     if (!std::isfinite(eps) || eps < 0.0 || eps >= 1.0) return set_error(ACP_EINVAL, "eps=%g outside [0, 1)", eps);
     if (eps > 0.0) {
         if (L_max < 1 || L_max > (INT64_C(1) << 31))

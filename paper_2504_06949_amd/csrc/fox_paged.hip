@@ -12,9 +12,12 @@
 //                       16 in a sequence (single tokens above all): the waves take different
 //                       pages of the same rows.  Bound by memory: a page is read once for
 //                       all query heads that share it.
-// Where rows are few, a sequence's kept pages are divided among several workgroups, whose
-// partial sums paged_join_kernel merges (a launch of its own orders them without a
-// device-wide fence).
+// The kept pages of all (rows, head) items, one after the other, are dealt in equal shares to
+// as many workgroups as the chip holds at a time, whatever lengths and heads they belong to:
+// paged_plan_kernel finds each item's pages, every workgroup adds up where its share lies,
+// and paged_join_kernel merges the sums of items that lie in several shares (launches of
+// their own order these without a device-wide fence).  Where items are many times the
+// workgroups, or have a few pages only, a workgroup takes an item instead.
 #include <type_traits>
 
 #include "acp_paged.h"
@@ -24,7 +27,6 @@ namespace acp {
 namespace {
 
 constexpr int kShortRows = 16;    // rows of a short sequence: new tokens times query heads
-constexpr int kMaxSplit = 64;     // parts of a row's keys (a lane each in the merge)
 constexpr float kSlack = 8.f;     // a weight is at most 2^8
 
 __device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) {
@@ -76,13 +78,13 @@ struct RowBlock {
         for (int s = 0; s < NK; ++s)
             q[qt][s] = *reinterpret_cast<const Frag*>(row + 4 * kFrag * s + kFrag * g);
     }
-    // s[kk][qt] = init[qt] + K Q^T of subtile kk; k(kk, piece) gives the lane's A operand
+    // s[kk][qt] = K Q^T of subtile kk; k(kk, piece) gives the lane's A operand
     template <typename F>
-    __device__ __forceinline__ void scores(f32x4 (&s)[2][NQ], const float (&init)[NQ], F k) const {
+    __device__ __forceinline__ void scores(f32x4 (&s)[2][NQ], F k) const {
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
 #pragma unroll
-            for (int qt = 0; qt < NQ; ++qt) s[kk][qt] = f32x4{init[qt], init[qt], init[qt], init[qt]};
+            for (int qt = 0; qt < NQ; ++qt) s[kk][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int p = 0; p < NK; ++p) {
                 const Frag a = k(kk, p);
@@ -153,6 +155,10 @@ struct RowBlock {
         }
     }
 };
+
+__device__ __forceinline__ float readlane_f32(float v, int l) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), l));
+}
 
 // Every lane's sum over the four lanes that hold a query
 __device__ __forceinline__ float over_groups(float v) {
@@ -252,22 +258,221 @@ __device__ __forceinline__ int first_page(const PagedArgs& a, int s, int h, int 
     return lo;
 }
 
+// ---- items and shares ------------------------------------------------------------------
+// An item: rows of a sequence that one head (short: one group of heads) takes over the pages
+// lo .. lo + pages - 1.
+struct Item {
+    int s;             // sequence, -1: no such item
+    int row0;          // first of its new rows
+    int lo, pages;
+};
+// The items of one kernel.  Item number (key head, tile, head of the group), in this order,
+// so that neighbouring shares read the same pages.
+struct Work {
+    Item* items;
+    bool shared;       // in shares; else a workgroup per item
+    int setup;         // what taking up an item costs, in pages: its place in the list is that
+                       // much longer than its pages, in front of them
+    long long* start;  // [n + 1] where the items' places begin (written by workgroup 0)
+    float* slots;      // [2 wgs] partial sums of a share's first item and of a later one
+    int n, tiles;      // items; tiles of all sequences together, at most
+    int wgs, least;    // workgroups; the least pages of a share
+};
+
+// Pages from lo up to those that the table has, for rows up to position last
+__device__ __forceinline__ int page_count(const PagedArgs& a, int lo, int last) {
+    return max(min(last >> 6, a.W - 1) - lo + 1, 0);
+}
+__device__ __forceinline__ double gate_at(const PagedArgs& a, int s, int h, int pos) {
+    const int p = page_of(a, s, pos >> 6);
+    return p < 0 ? 0.0 : gates_of(a, p, h)[pos & 63];
+}
+// 0, which the compiler does not know: what is rarely computed from it is not computed ahead
+// of a loop and kept
+__device__ __forceinline__ int late_zero() {
+    int z = 0;
+    asm volatile("" : "+s"(z));
+    return z;
+}
+// A kernel's first argument, read anew where it is used, for the same reason
+__device__ __forceinline__ const PagedArgs& late_args() {
+    typedef const __attribute__((address_space(4))) char* KernargPtr;
+    return *(const PagedArgs*)((KernargPtr)__builtin_amdgcn_kernarg_segment_ptr() + late_zero());
+}
+__device__ __forceinline__ void report(const PagedArgs& a, int s, int h, int lane) {
+    if (a.flags && lane == 0) atomicOr(a.flags + (int64_t)(s + late_zero()) * a.H + h, kFlagPage);
+}
+
+// The same in every lane, and known to be
+__device__ __forceinline__ Seq uniform_seq(const PagedArgs& a, int s) {
+    const Seq q = seq_of(a, s);
+    return Seq{__builtin_amdgcn_readfirstlane(q.row0), __builtin_amdgcn_readfirstlane(q.n),
+               __builtin_amdgcn_readfirstlane(q.past)};
+}
+
+// Long item `id` and its head, by a wave
+template <int kRows>
+__device__ __forceinline__ Item long_item(const PagedArgs& a, int id, int tiles, int short_max, int lane) {
+    const int G = a.H / a.Hk, hk = id / (tiles * G), rest = id - hk * tiles * G;
+    const int h = hk * G + rest % G;
+    Item it{-1, 0, 0, 0};
+    int tile;
+    // (the last tiles of a sequence have the most pages: they go first)
+    if (!locate(a, tiles - 1 - rest / G, kRows, short_max, 0x7fffffff, lane, it.s, tile)) {
+        it.s = -1;
+        return it;
+    }
+    const Seq q = seq_of(a, it.s);
+    it.row0 = tile * kRows;
+    const int p0 = q.past + it.row0, p1 = p0 + min(kRows, q.n - it.row0) - 1;
+    it.lo = first_page(a, it.s, h, p0 >> 6, readfirst_f64(gate_at(a, it.s, h, p0)),
+                       readfirst_f64(head_delta(a, h)), lane);
+    it.pages = page_count(a, it.lo, p1);
+    if ((p1 >> 6) >= a.W) report(a, it.s, h, lane);
+    return it;
+}
+__device__ __forceinline__ int long_head(const PagedArgs& a, int id, int tiles) {
+    const int G = a.H / a.Hk, hk = id / (tiles * G);
+    return hk * G + (id - hk * tiles * G) % G;
+}
+
+// Short item `id`, by kWaves waves: the first page that any head of the group keeps for the
+// first token
+template <int kWaves>
+__device__ __forceinline__ Item short_item(const PagedArgs& a, int id, int tiles, int short_max, int wave,
+                                           int lane, int (&first)[16]) {
+    const int G = a.H / a.Hk, hk = id / tiles;
+    Item it{-1, 0, 0, 0};
+    int tile;
+    if (!locate(a, id - hk * tiles, short_max, 0, short_max, lane, it.s, tile)) {
+        it.s = -1;
+        return it;                                   // (every wave alike)
+    }
+    const Seq q = seq_of(a, it.s);
+    const int last = q.past + q.n - 1;
+    for (int k = wave; k < G; k += kWaves) {
+        const int h = hk * G + k;
+        const int f = first_page(a, it.s, h, q.past >> 6, readfirst_f64(gate_at(a, it.s, h, q.past)),
+                                 readfirst_f64(head_delta(a, h)), lane);
+        if (lane == 0) first[k] = f;
+        if ((last >> 6) >= a.W) report(a, it.s, h, lane);
+    }
+    __syncthreads();
+    it.lo = first[0];
+    for (int k = 1; k < G; ++k) it.lo = min(it.lo, first[k]);
+    it.pages = page_count(a, it.lo, last);
+    return it;
+}
+
+// The items of both kernels: 8 long ones, or a short one, per workgroup of 8 waves
+template <int kRows>
+__global__ __launch_bounds__(512) void paged_plan_kernel(PagedArgs a, Work lw, Work sw, int short_max,
+                                                         int long_above) {
+    __shared__ int first[16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int nl = (lw.n + 7) / 8;
+    if ((int)blockIdx.x < nl) {
+        const int id = blockIdx.x * 8 + wave;
+        if (id >= lw.n) return;
+        const Item it = long_item<kRows>(a, id, lw.tiles, long_above, lane);
+        if (lane == 0) lw.items[id] = it;
+    } else {
+        const int id = blockIdx.x - nl;
+        const Item it = short_item<8>(a, id, sw.tiles, short_max, wave, lane, first);
+        if (threadIdx.x == 0) sw.items[id] = it;
+    }
+}
+
+__device__ __forceinline__ int place_of(const Work& w, int pages) { return pages > 0 ? pages + w.setup : 0; }
+
+// A workgroup's share: `left` of the list from `skip` in item `item`'s place on
+struct Share {
+    int item, skip, left;
+    bool later;        // past the share's first item
+};
+struct ShareSmem {
+    long long wave[4];
+    int item, skip, left;
+};
+// The share of workgroup wg (256 threads); left = 0: none.  Workgroup 0 also writes the list
+// of starts for the merge.  A share fits an int: fewer than 8 items per workgroup are shared
+// out, to at least kLeastShares, of at most 2^25 pages each.
+__device__ __forceinline__ Share find_share(const Work& w, int wg, ShareSmem& sm) {
+    if (!w.shared) return Share{wg, 0, 0x7fffffff, false};        // the item, whole
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const int per = (w.n + 255) / 256, i0 = min(t * per, w.n), i1 = min(i0 + per, w.n);
+    long long sum = 0;
+    for (int i = i0; i < i1; ++i) sum += place_of(w, w.items[i].pages);
+    long long incl = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const long long u = __shfl_up(incl, o);
+        if (lane >= o) incl += u;
+    }
+    if (lane == 63) sm.wave[wave] = incl;
+    if (t == 0) sm.left = 0;
+    __syncthreads();
+    long long total = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (k < wave) incl += sm.wave[k];
+        total += sm.wave[k];
+    }
+    long long before = incl - sum;
+    if (wg == 0) {
+        long long b = before;
+        for (int i = i0; i < i1; ++i) {
+            w.start[i] = b;
+            b += place_of(w, w.items[i].pages);
+        }
+        if (t == 255) w.start[w.n] = total;
+    }
+    const long long chunk = max((total + w.wgs - 1) / w.wgs, (long long)w.least), at = wg * chunk;
+    if (at < total && before <= at && at < incl) {       // (one thread: its items hold pages)
+        int i = i0;
+        for (; before + place_of(w, w.items[i].pages) <= at; ++i) before += place_of(w, w.items[i].pages);
+        sm.item = i;
+        sm.skip = (int)(at - before);
+        sm.left = (int)min(chunk, total - at);
+    }
+    __syncthreads();
+    return Share{__builtin_amdgcn_readfirstlane(sm.item), __builtin_amdgcn_readfirstlane(sm.skip),
+                 __builtin_amdgcn_readfirstlane(sm.left), false};
+}
+// The share's pages of its present item: first, count (0: the share ends in front of them)
+__device__ __forceinline__ int pages_here(const Work& w, const Share& sh, const Item& it, int& first) {
+    const int setup = w.shared ? w.setup : 0;
+    first = it.lo + max(sh.skip - setup, 0);
+    return min(max(sh.left - max(setup - sh.skip, 0), 0), it.lo + it.pages - first);
+}
+// On to the share's next item that has pages; false at its end
+__device__ __forceinline__ bool next_item(const Work& w, Share& sh, const Item& it) {
+    sh.left -= place_of(w, it.pages) - sh.skip;
+    if (!w.shared || sh.left <= 0) return false;
+    sh.skip = 0;
+    sh.later = true;
+    do ++sh.item;
+    while (__builtin_amdgcn_readfirstlane(w.items[sh.item].pages) == 0);
+    return true;
+}
+__device__ __forceinline__ Item item_at(const Work& w, int i) {
+    const Item t = w.items[i];
+    return Item{__builtin_amdgcn_readfirstlane(t.s), __builtin_amdgcn_readfirstlane(t.row0),
+                __builtin_amdgcn_readfirstlane(t.lo), __builtin_amdgcn_readfirstlane(t.pages)};
+}
+
 // Page numbers of 64 consecutive pages, one per lane
 struct PageWindow {
     int base, id;
     __device__ __forceinline__ void fill(const PagedArgs& a, int s, int n, int lane) {
         base = n;
-        id = page_of(a, s, n + lane);
+        id = page_of(a, s + late_zero(), n + lane);
     }
     __device__ __forceinline__ int get(const PagedArgs& a, int s, int n, int lane) {
         if (n - base >= 64) fill(a, s, n, lane);
         return __builtin_amdgcn_readlane(id, n - base);
     }
 };
-
-__device__ __forceinline__ void report(const PagedArgs& a, int s, int h, int lane) {
-    if (a.flags && lane == 0) atomicOr(a.flags + (int64_t)s * a.H + h, kFlagPage);
-}
 
 // ---- tiles of 64 rows in LDS -----------------------------------------------------------
 // bf16: the swizzled panels of acp_device.h.  float: rows of D, 16-byte chunk c of row r at
@@ -336,41 +541,28 @@ __device__ __forceinline__ void clean_values(unsigned char* tile, int valid, uns
     }
 }
 
-// Workgroup -> (head, item).  Workgroups go to the 8 XCDs in turn; each XCD takes every
-// eighth item of every head, heads fastest.  Heads keep different numbers of pages, and
-// this gives each XCD the same share of each; the workgroups at work on an XCD at one time
-// are neighbouring items of all heads, so that those that read the same pages share its L2.
-__device__ __forceinline__ void deal(int heads, int& h, int& item) {
-    const int x = blockIdx.x & 7, k = blockIdx.x >> 3;
-    h = k % heads;
-    item = k / heads * 8 + x;
-}
-__host__ inline unsigned dealt(int64_t items, int heads) { return (unsigned)((items + 7) / 8 * 8 * heads); }
-
-// Row t, head h of the output, or its share of the part `sp` of `splits`
+// A row's result: to the output, or to row r of a slot for R rows
 template <typename T, int D>
-__device__ __forceinline__ void put_row(const PagedArgs& a, int t, int h, int sp, int splits, int stride,
-                                        const f32x4 (&acc)[D / 16], float m, float l, int g) {
+__device__ __forceinline__ void put_row(const PagedArgs& a, int t, int h, const f32x4 (&acc)[D / 16], float m,
+                                        float l, int g) {
     const int64_t row = (int64_t)t * a.H + h;
-    if (splits == 1) {
-        const float inv = l == 0.f ? 0.f : 1.0f / l;     // (no key: every page was bad)
+    const float inv = l == 0.f ? 0.f : 1.0f / l;         // (no key: every page was bad)
 #pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt) {
-            T o[4];
+    for (int dt = 0; dt < D / 16; ++dt) {
+        T o[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) o[k] = from_f32<T>(acc[dt][k] * inv);
-            __builtin_memcpy((T*)a.O + row * D + 16 * dt + 4 * g, o, sizeof(o));
-        }
-        if (g == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + fast_log2(l)) * kLn2;
-    } else {
-        float2* ml = reinterpret_cast<float2*>(a.part) + row * stride;
-        float* po = a.part + 2 * (int64_t)a.T * a.H * stride + (row * stride + sp) * D;
-        if (g == 0) ml[sp] = make_float2(m, l);
-        if (m > -INFINITY || m != m)
-#pragma unroll
-            for (int dt = 0; dt < D / 16; ++dt)
-                *reinterpret_cast<f32x4*>(po + 16 * dt + 4 * g) = acc[dt];
+        for (int k = 0; k < 4; ++k) o[k] = from_f32<T>(acc[dt][k] * inv);
+        __builtin_memcpy((T*)a.O + row * D + 16 * dt + 4 * g, o, sizeof(o));
     }
+    if (g == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + fast_log2(l)) * kLn2;
+}
+template <int D>
+constexpr int slot_floats(int rows) { return rows * (D + 2); }
+template <int D, int R>
+__device__ __forceinline__ void put_part(float* slot, int r, const f32x4 (&acc)[D / 16], float m, float l, int g) {
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) *reinterpret_cast<f32x4*>(slot + r * D + 16 * dt + 4 * g) = acc[dt];
+    if (g == 0) *reinterpret_cast<float2*>(slot + R * D + 2 * r) = make_float2(m, l);
 }
 
 // ---- long ------------------------------------------------------------------------------
@@ -381,44 +573,46 @@ struct alignas(1024) LongSmem {
     float kb[2][64];         // (c_j - R) log2(e), negated
     float2 kd[2][64];        // c_j - R as a sum of two floats
     double end[2];           // c of the page's last position
+    double rc[64 * NQ];      // c_i of the rows
+    float2 rd[64 * NQ];      // c_i - R likewise
     unsigned bad[2][2];      // keys of the page with values that are not finite
     unsigned inf[64 * NQ][2][D / 32];
     int marked;
+    ShareSmem share;
 };
 
 template <typename T, int D, int NQ>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 && is_bf16<T>() ? 3 : 2)))
-void paged_long_kernel(PagedArgs a, int tiles, int splits, int stride, int short_max, float kscale) {
+void paged_long_kernel(PagedArgs, Work work, float kscale) {
     constexpr int kRows = 64 * NQ;
     typedef RowBlock<T, D, NQ> Block;
     __shared__ LongSmem<T, D, NQ> sm;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63, g = lane >> 4, r16 = lane & 15;
-    int h, rest;
-    deal(a.H, h, rest);
-    const int sp = rest % splits;
-    if (rest / splits >= tiles) return;
-    int s, tile;
-    // (the last tiles of a sequence have the most pages: they go first)
-    if (!locate(a, tiles - 1 - rest / splits, kRows, short_max, 0x7fffffff, lane, s, tile)) return;
-    const Seq q = seq_of(a, s);
+    const int wg = blockIdx.x;
+    Share sh = find_share(work, wg, sm.share);
+    if (sh.left == 0) return;
+    for (;;) {
+    // (recomputed for each item: held across the loop, what depends on them costs registers)
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    const int lane = tid & 63, g = lane >> 4, r16 = lane & 15;
+    const PagedArgs& a = late_args();
+    const Item it = item_at(work, sh.item);
+    if (it.s < 0) return;                               // (not in a share)
+    const int s = it.s, row0 = it.row0, h = long_head(a, sh.item, work.tiles);
+    // this share's pages of the item
+    int nb;
+    const int taken = pages_here(work, sh, it, nb), ne = nb + taken - 1;
+    if (work.shared && taken == 0) return;
+    const Seq q = uniform_seq(a, s);
     const int hk = h / (a.H / a.Hk);
     const double delta = readfirst_f64(head_delta(a, h));
-    const int row0 = tile * kRows, rows = min(kRows, q.n - row0);    // of the sequence's new rows
+    const int rows = min(kRows, q.n - row0);                         // of the sequence's new rows
     const int p0 = q.past + row0, p1 = p0 + rows - 1;                // positions of the tile
     const int len = q.past + q.n;
-    const int nd1 = p1 >> 6;
 
-    auto gate = [&](int pos) __attribute__((always_inline)) {
-        const int p = page_of(a, s, pos >> 6);
-        return p < 0 ? 0.0 : gates_of(a, p, h)[pos & 63];
-    };
+    auto gate = [&](int pos) __attribute__((always_inline)) { return gate_at(a, s, h, pos); };
     const double R = readfirst_f64(gate(p0));
-    const int lo = first_page(a, s, h, p0 >> 6, R, delta, lane);
-    // this part's pages, of those the table has (the last one there may be is W - 1)
-    const int top = min(nd1, a.W - 1), pages = max(top - lo + 1, 0), per = (pages + splits - 1) / splits;
-    const int nb = lo + sp * per, ne = min(nb + per - 1, top);
-    if (nd1 >= a.W && wave == 0) report(a, s, h, lane);
 
     Block blk;
     blk.clear();
@@ -427,48 +621,48 @@ void paged_long_kernel(PagedArgs a, int tiles, int splits, int stride, int short
     const int o0 = 16 * NQ * wave;
     const bool wave_on = o0 < rows;
     const int w0 = p0 + min(o0, rows - 1), w1 = p0 + min(o0 + 16 * NQ - 1, rows - 1);
-    double ci[NQ];
-    int pi[NQ];
-    float2 rd[NQ];                                                   // c_i - R likewise
-    float init[NQ], zero[NQ];                                        // start of the scores
-    const float per_y = sqrtf((float)D) * kLn2;                      // q.k per unit of y
+    auto pos_of = [&](int qt) __attribute__((always_inline)) { return p0 + min(o0 + 16 * qt + r16, rows - 1); };
+    float row[NQ];                                                   // (c_i - R) log2(e) - ref
 #pragma unroll
     for (int qt = 0; qt < NQ; ++qt) {
-        pi[qt] = p0 + min(o0 + 16 * qt + r16, rows - 1);
-        ci[qt] = gate(pi[qt]);
-        blk.load_q(qt, (const T*)a.q + (int64_t)(q.row0 + pi[qt] - q.past) * a.qt + (int64_t)h * a.qh, g);
-        const double r = ci[qt] - R;
-        rd[qt].x = (float)r;
-        rd[qt].y = (float)(r - (double)rd[qt].x);
-        init[qt] = rd[qt].x * (kLog2e * per_y);
-        zero[qt] = 0.f;
+        const int pos = pos_of(qt), i = o0 + 16 * qt + r16;
+        const double ci = gate(pos), r = ci - R;
+        blk.load_q(qt, (const T*)a.q + (int64_t)(q.row0 + pos - q.past) * a.qt + (int64_t)h * a.qh, g);
+        // (the wave's own rows: no other reads them)
+        const float hi = (float)r;
+        sm.rc[i] = ci;
+        sm.rd[i] = make_float2(hi, (float)(r - (double)hi));
+        row[qt] = hi * kLog2e;
     }
-    const double c_first = readfirst_f64(ci[0]);
+    const double c_first = readfirst_f64(gate(w0));
     const double c_tile_last = readfirst_f64(gate(p1));
 
     PageDma<T, D> dma;
     dma.init(wave, lane);
     PageWindow win;
-    const T* kp = (const T*)a.kp;
-    const T* vp = (const T*)a.vp;
+    // (all that the loops need of the arguments)
+    const T* kp = (const T*)a.kp + (int64_t)hk * 64 * D;
+    const T* vp = (const T*)a.vp + (int64_t)hk * 64 * D;
+    const double* gates = a.cp + (int64_t)h * 64;
+    const int64_t page_stride = (int64_t)a.Hk * 64 * D, gate_stride = (int64_t)a.H * 64;
     double cn = 0.0;                        // the next page's gate, thread t < 64
     int page_next = -1;                     // the page last asked for, -1: not in the cache
     auto issue = [&](int n, int buf) __attribute__((always_inline)) {
         const int p = win.get(a, s, n, lane);
-        const int64_t at = ((int64_t)max(p, 0) * a.Hk + hk) * 64 * D;
+        const int64_t at = max(p, 0) * page_stride;
         page_next = p;
-        if (threadIdx.x < 64) cn = gates_of(a, max(p, 0), h)[threadIdx.x];
+        if (tid < 64) cn = gates[(int64_t)max(p, 0) * gate_stride + tid];
         dma.issue(sm.k[buf], kp + at, wave);
         dma.issue(sm.v[buf], vp + at, wave);
     };
     auto put_gates = [&](int buf) __attribute__((always_inline)) {
-        if (threadIdx.x < 64) {
+        if (tid < 64) {
             const double r = cn - R;
             const float hi = (float)r;
-            sm.kb[buf][threadIdx.x] = -hi * kLog2e;
-            sm.kd[buf][threadIdx.x] = make_float2(hi, (float)(r - (double)hi));
-            if (threadIdx.x == 63) sm.end[buf] = cn;
-            if (threadIdx.x < 2) sm.bad[buf][threadIdx.x] = 0;
+            sm.kb[buf][tid] = -hi * kLog2e;
+            sm.kd[buf][tid] = make_float2(hi, (float)(r - (double)hi));
+            if (tid == 63) sm.end[buf] = cn;
+            if (tid < 2) sm.bad[buf][tid] = 0;
         }
     };
 
@@ -489,43 +683,83 @@ void paged_long_kernel(PagedArgs a, int tiles, int splits, int stride, int short
         if constexpr (kMask) {
             const double end = sm.end[buf];
 #pragma unroll
-            for (int qt = 0; qt < NQ; ++qt) keep[qt] = n >= (pi[qt] >> 6) || ci[qt] - end >= delta;
+            for (int qt = 0; qt < NQ; ++qt)
+                keep[qt] = n >= (pos_of(qt) >> 6) || sm.rc[o0 + 16 * qt + r16] - end >= delta;
         }
+        // LDS operands are asked for together (bf16): all keys of a half before its first
+        // product, its values before its weights are formed.  The scheduling barriers keep the
+        // reads there: left to itself the compiler reads each operand just before its product
+        // and waits.
+        constexpr bool kAhead = is_bf16<T>() && !kMask;
+        typename Block::Frag kf[2][Block::NK];
+        auto load_keys = [&](int ks) __attribute__((always_inline)) {
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                for (int p = 0; p < Block::NK; ++p) {
+                    // (subtile kk of half ks starts 32 ks + 4 kk (float: 16 kk) rows further: the
+                    // swizzle of the lane's rows stays the same)
+                    const int o = is_bf16<T>() ? 128 * (32 * ks + 4 * kk) : D * 4 * (32 * ks + 16 * kk);
+                    kf[kk][p] = *reinterpret_cast<const typename Block::Frag*>(sm.k[buf] + koff[p] + o);
+                }
+        };
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             f32x4 x[2][NQ];
+            load_keys(ks);
+            if constexpr (is_bf16<T>()) __builtin_amdgcn_sched_barrier(0);
+            blk.scores(x, [&](int kk, int p) __attribute__((always_inline)) { return kf[kk][p]; });
             __builtin_amdgcn_sched_barrier(0);
-            blk.scores(x, kMask ? zero : init, [&](int kk, int p) __attribute__((always_inline)) {
-                // (subtile kk of half ks starts 32 ks + 4 kk (float: 16 kk) rows further: the
-                // swizzle of the lane's rows stays the same)
-                const int o = is_bf16<T>() ? 128 * (32 * ks + 4 * kk) : D * 4 * (32 * ks + 16 * kk);
-                return *reinterpret_cast<const typename Block::Frag*>(sm.k[buf] + koff[p] + o);
-            });
-            __builtin_amdgcn_sched_barrier(0);
-            float p[NQ][8];
+            bf16x8 vf[is_bf16<T>() ? Block::ND : 1];
+            auto load_values = [&]() __attribute__((always_inline)) {
+                if constexpr (is_bf16<T>()) {
 #pragma unroll
-            for (int qt = 0; qt < NQ; ++qt) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int key = 32 * ks + key_of<T>(g, j);
-                    float y;
-                    if constexpr (kMask) {
-                        const float2 kd = sm.kd[buf][key];
-                        const float decay = (rd[qt].x - kd.x) + (rd[qt].y - kd.y);
-                        y = __builtin_fmaf(x[j >> 2][qt][j & 3], kscale,
-                                           __builtin_fmaf(decay, kLog2e, -blk.ref[qt]));
-                        if (!keep[qt] || 64 * n + key > pi[qt]) y = -INFINITY;
-                    } else {
-                        y = __builtin_fmaf(x[j >> 2][qt][j & 3], kscale, sm.kb[buf][key]);
-                    }
-                    p[qt][j] = y;
+                    for (int dt = 0; dt < Block::ND; ++dt) vf[dt] = tile_col8_at(sm.v[buf] + voff[dt] + 128 * 32 * ks);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                if (blk.weights(qt, p[qt])) init[qt] = __builtin_fmaf(rd[qt].x, kLog2e, -blk.ref[qt]) * per_y;
+            };
+            if constexpr (kAhead) load_values();
+            float p[NQ][8];
+            if constexpr (kMask) {
+                float2 kd[8], rd[NQ];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) kd[j] = sm.kd[buf][32 * ks + key_of<T>(g, j)];
+#pragma unroll
+                for (int qt = 0; qt < NQ; ++qt) rd[qt] = sm.rd[o0 + 16 * qt + r16];
+                // (held here: read where they are used, each read would stand in a branch of its own)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) asm volatile("" : "+v"(kd[j].x), "+v"(kd[j].y));
+#pragma unroll
+                for (int qt = 0; qt < NQ; ++qt) {
+                    // keys up to `last` of the half
+                    const int last = keep[qt] ? pos_of(qt) - 64 * n - 32 * ks : -1;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float decay = (rd[qt].x - kd[j].x) + (rd[qt].y - kd[j].y);
+                        const float y = __builtin_fmaf(x[j >> 2][qt][j & 3], kscale,
+                                                       __builtin_fmaf(decay, kLog2e, -blk.ref[qt]));
+                        p[qt][j] = key_of<T>(g, j) <= last ? y : -INFINITY;
+                    }
+                }
+            } else {
+                float kb[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) kb[j] = sm.kb[buf][32 * ks + key_of<T>(g, j)];
+#pragma unroll
+                for (int qt = 0; qt < NQ; ++qt)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        p[qt][j] = __builtin_fmaf(x[j >> 2][qt][j & 3], kscale, kb[j] + row[qt]);
             }
+#pragma unroll
+            for (int qt = 0; qt < NQ; ++qt)
+                if (blk.weights(qt, p[qt]))
+                    row[qt] = __builtin_fmaf(sm.rd[o0 + 16 * qt + r16].x, kLog2e, -blk.ref[qt]);
             __builtin_amdgcn_sched_barrier(0);
+            if constexpr (!kAhead) load_values();
             blk.add(p, [&](int dt, int j) __attribute__((always_inline)) {
                 if constexpr (is_bf16<T>())
-                    return tile_col8_at(sm.v[buf] + voff[dt] + 128 * 32 * ks);
+                    return vf[dt];
                 else
                     return *reinterpret_cast<const float*>(
                         sm.v[buf] + f32_off<D>(32 * ks + key_of<T>(g, j), 16 * dt + r16));
@@ -534,8 +768,8 @@ void paged_long_kernel(PagedArgs a, int tiles, int splits, int stride, int short
         __builtin_amdgcn_sched_barrier(0);
     };
 
-    if (threadIdx.x == 0) sm.marked = 0;
-    for (int i = threadIdx.x; i < 64 * NQ * 2 * (D / 32); i += 256) (&sm.inf[0][0][0])[i] = 0;
+    if (tid == 0) sm.marked = 0;
+    for (int i = tid; i < 64 * NQ * 2 * (D / 32); i += 256) (&sm.inf[0][0][0])[i] = 0;
     if (nb <= ne) {
         win.fill(a, s, nb, lane);
         issue(nb, 0);
@@ -551,7 +785,7 @@ void paged_long_kernel(PagedArgs a, int tiles, int splits, int stride, int short
             if (n < ne) issue(n + 1, buf ^ 1);
             unsigned long long bad = 0;
             if (kMask && page >= 0) {
-                clean_values<T, D>(sm.v[buf], len - 64 * n, sm.bad[buf], threadIdx.x, 256);
+                clean_values<T, D>(sm.v[buf], len - 64 * n, sm.bad[buf], tid, 256);
                 lds_barrier();
                 bad = (unsigned long long)sm.bad[buf][1] << 32 | sm.bad[buf][0];
             }
@@ -564,7 +798,7 @@ void paged_long_kernel(PagedArgs a, int tiles, int splits, int stride, int short
                 for (int qt = 0; qt < NQ; ++qt) {
                     const int pos = p0 + min(o0 + 16 * qt + r16, rows - 1);
                     if (o0 + 16 * qt + r16 < rows && (n >= (pos >> 6) || gate(pos) - sm.end[buf] >= delta))
-                        mark_bad<T, D>(bad, vp + ((int64_t)page * a.Hk + hk) * 64 * D, 64 * n, pos, lane,
+                        mark_bad<T, D>(bad, vp + page * page_stride, 64 * n, pos, lane,
                                        sm.inf[16 * (NQ * wave + qt) + r16]);
                 }
             }
@@ -581,13 +815,20 @@ void paged_long_kernel(PagedArgs a, int tiles, int splits, int stride, int short
             while (n <= ne && partly()) next(std::true_type{});
         }
     }
-    if (!wave_on) return;
+    if (wave_on) {
+        float* slot = work.slots + (int64_t)(2 * wg + sh.later) * slot_floats<D>(kRows);
 #pragma unroll
-    for (int qt = 0; qt < NQ; ++qt) {
-        const float l = over_groups(blk.l[qt]);
-        if (o0 + 16 * qt + r16 >= rows) continue;
-        if (nb <= ne && sm.marked) add_marks<D>(blk.acc[qt], sm.inf[16 * (NQ * wave + qt) + r16], g);
-        put_row<T, D>(a, q.row0 + pi[qt] - q.past, h, sp, splits, stride, blk.acc[qt], blk.max_logit(qt), l, g);
+        for (int qt = 0; qt < NQ; ++qt) {
+            const float l = over_groups(blk.l[qt]);
+            const int r = o0 + 16 * qt + r16;
+            if (r >= rows) continue;
+            if (nb <= ne && sm.marked) add_marks<D>(blk.acc[qt], sm.inf[r], g);
+            if (taken == it.pages) put_row<T, D>(a, q.row0 + row0 + r, h, blk.acc[qt], blk.max_logit(qt), l, g);
+            else put_part<D, kRows>(slot, r, blk.acc[qt], blk.max_logit(qt), l, g);
+        }
+    }
+    if (!next_item(work, sh, it)) return;
+    __syncthreads();                                    // (the marks are read)
     }
 }
 
@@ -601,26 +842,34 @@ struct alignas(1024) ShortSmem {
     int marked;
     float m[4][16], l[4][16];
     int first[16];
+    ShareSmem share;
 };
 
 // Rows r = token * G + head of the group, r < 16, are the queries of every wave.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void paged_short_kernel(PagedArgs a, int splits, int stride, int short_max,
-                                                          float kscale) {
+__global__ __launch_bounds__(256) void paged_short_kernel(PagedArgs, Work work, float kscale) {
     typedef RowBlock<T, D, 1> Block;
     constexpr int KH = is_bf16<T>() ? 2 : 1;            // halves of 32 keys per step
     constexpr int ND = D / 16;
     __shared__ ShortSmem<T, D> sm;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63, g = lane >> 4, r16 = lane & 15;
-    int hk, rest;
-    deal(a.Hk, hk, rest);
-    const int sp = rest % splits;
-    int s, tile;
-    if (!locate(a, rest / splits, short_max, 0, short_max, lane, s, tile)) return;
-    const Seq q = seq_of(a, s);
+    const int wg = blockIdx.x;
+    Share sh = find_share(work, wg, sm.share);
+    if (sh.left == 0) return;
+    for (;;) {
+    const PagedArgs& a = late_args();
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    const int lane = tid & 63, g = lane >> 4, r16 = lane & 15;
+    const Item it = item_at(work, sh.item);
+    if (it.s < 0) return;                               // (not in a share)
+    const int s = it.s, hk = sh.item / work.tiles;
+    int nb;
+    const int taken = pages_here(work, sh, it, nb), ne = nb + taken - 1;
+    if (work.shared && taken == 0) return;
+    const Seq q = uniform_seq(a, s);
     const int G = a.H / a.Hk, nrows = q.n * G;
-    const int len = q.past + q.n, nd1 = (len - 1) >> 6;
+    const int len = q.past + q.n;
     // the lane's row (those past the end repeat the last one)
     const int r = min(r16, nrows - 1);
     const int h = hk * G + r % G, pi = q.past + r / G;
@@ -631,23 +880,15 @@ __global__ __launch_bounds__(256) void paged_short_kernel(PagedArgs a, int split
     blk.clear();
     blk.load_q(0, (const T*)a.q + (int64_t)(q.row0 + r / G) * a.qt + (int64_t)h * a.qh, g);
 
-    // first page that any row keeps: rows 0 .. G - 1 are the first token's
-    for (int k = wave; k < G; k += 4) {
-        const double ck = readlane_f64(ci, k), dk = readlane_f64(delta, k);
-        const int f = first_page(a, s, hk * G + k, q.past >> 6, ck, dk, lane);
-        if (lane == 0) sm.first[k] = f;
-    }
-    if (threadIdx.x == 0) sm.marked = 0;
-    for (int i = threadIdx.x; i < 16 * 2 * (D / 32); i += 256) (&sm.inf[0][0][0])[i] = 0;
+    if (tid == 0) sm.marked = 0;
+    for (int i = tid; i < 16 * 2 * (D / 32); i += 256) (&sm.inf[0][0][0])[i] = 0;
     __syncthreads();
-    int lo = sm.first[0];
-    for (int k = 1; k < G; ++k) lo = min(lo, sm.first[k]);
-    const int top = min(nd1, a.W - 1), pages = max(top - lo + 1, 0), per = (pages + splits - 1) / splits;
-    const int nb = lo + sp * per, ne = min(nb + per - 1, top);
-    if (nd1 >= a.W && r16 < nrows) report(a, s, h, lane & 48);
 
-    const T* kp = (const T*)a.kp;
-    const T* vp = (const T*)a.vp;
+    // (all that the loops need of the arguments)
+    const T* kp = (const T*)a.kp + (int64_t)hk * 64 * D;
+    const T* vp = (const T*)a.vp + (int64_t)hk * 64 * D;
+    const double* gates = a.cp + (int64_t)h * 64;         // of the lane's head
+    const int64_t page_stride = (int64_t)a.Hk * 64 * D, gate_stride = (int64_t)a.H * 64;
     // What a step needs, requested one step ahead (bf16) or at its start (float)
     typename Block::Frag kf[KH][2][Block::NK];
     double cj[KH][8], cend = 0.0;
@@ -660,8 +901,8 @@ __global__ __launch_bounds__(256) void paged_short_kernel(PagedArgs a, int split
     auto load = [&](int n, int hf, int buf) __attribute__((always_inline)) {
         const int p = win.get(a, s, n, lane);
         page = p;
-        const int64_t at = ((int64_t)max(p, 0) * a.Hk + hk) * 64 * D;
-        const double* cp = gates_of(a, max(p, 0), h);
+        const int64_t at = max(p, 0) * page_stride;
+        const double* cp = gates + max(p, 0) * gate_stride;
 #pragma unroll
         for (int ks = 0; ks < KH; ++ks) {
 #pragma unroll
@@ -755,8 +996,7 @@ __global__ __launch_bounds__(256) void paged_short_kernel(PagedArgs a, int split
 #pragma unroll
         for (int ks = 0; ks < KH; ++ks) {
             f32x4 x[2][1];
-            const float zero[1] = {0.f};
-            blk.scores(x, zero, [&](int kk, int i) __attribute__((always_inline)) { return kc[ks][kk][i]; });
+            blk.scores(x, [&](int kk, int i) __attribute__((always_inline)) { return kc[ks][kk][i]; });
             float p[1][8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -775,7 +1015,7 @@ __global__ __launch_bounds__(256) void paged_short_kernel(PagedArgs a, int split
         if (bad) {
             sm.marked = 1;
             if (keep && r16 < nrows)
-                mark_bad<T, D>(bad, vp + ((int64_t)pg * a.Hk + hk) * 64 * D, 64 * n, pi, lane, sm.inf[r16]);
+                mark_bad<T, D>(bad, vp + pg * page_stride, 64 * n, pi, lane, sm.inf[r16]);
         }
     }
 
@@ -799,63 +1039,111 @@ __global__ __launch_bounds__(256) void paged_short_kernel(PagedArgs a, int split
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) o_s[wave - 1][dt][lane] = blk.acc[0][dt] * scale;
     __syncthreads();
-    if (wave > 0) return;
+    if (wave == 0) {
 #pragma unroll
-    for (int dt = 0; dt < ND; ++dt) {
-        f32x4 o = blk.acc[0][dt] * scale;
+        for (int dt = 0; dt < ND; ++dt) {
+            f32x4 o = blk.acc[0][dt] * scale;
 #pragma unroll
-        for (int w = 0; w < 3; ++w) o += o_s[w][dt][lane];
-        blk.acc[0][dt] = o;
+            for (int w = 0; w < 3; ++w) o += o_s[w][dt][lane];
+            blk.acc[0][dt] = o;
+        }
+        if (sm.marked) add_marks<D>(blk.acc[0], sm.inf[r16], g);
+        if (r16 < nrows) {
+            if (taken == it.pages) put_row<T, D>(a, q.row0 + r / G, h, blk.acc[0], M, L, g);
+            else put_part<D, 16>(work.slots + (int64_t)(2 * wg + sh.later) * slot_floats<D>(16), r16,
+                                 blk.acc[0], M, L, g);
+        }
     }
-    if (sm.marked) add_marks<D>(blk.acc[0], sm.inf[r16], g);
-    if (r16 < nrows) put_row<T, D>(a, q.row0 + r / G, h, sp, splits, stride, blk.acc[0], M, L, g);
+    if (!next_item(work, sh, it)) return;
+    __syncthreads();                                    // (the sums and marks are read)
+    }
 }
 
 // ---- merge -----------------------------------------------------------------------------
-// One wave per row: lane p takes part p's maximum and sum, then features lane, lane + 64.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a, int split_long, int split_short,
-                                                         int stride, int short_max, bool long_on) {
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    if (row >= (int64_t)a.T * a.H) return;
-    const int t = (int)(row / a.H);
-    int lo = 0, hi = a.N;                              // first s with cu[s + 1] > t
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (a.cu[mid + 1] > t) hi = mid;
-        else lo = mid + 1;
-    }
-    if (lo >= a.N) return;
-    const Seq q = seq_of(a, lo);
-    if (t < q.row0 || t >= q.row0 + q.n) return;
-    const bool is_short = q.n <= short_max;
-    if (!is_short && !long_on) return;
-    const int splits = is_short ? split_short : split_long;
-    if (splits == 1) return;                            // written already
-    const float2* ml = reinterpret_cast<const float2*>(a.part) + row * stride;
-    const float* po = a.part + 2 * (int64_t)a.T * a.H * stride + row * stride * D;
-    float2 v = make_float2(-INFINITY, 0.f);
-    if (lane < splits) v = ml[lane];
-    float M = v.x;
+// The partial sums of an item that lies in several shares, of R rows per slot; an item
+// without a page gets O = 0, lse = -inf.  A workgroup per item, the parts dealt to its waves
+// (kLong: per 16 rows, these dealt to them).
+template <typename T, int D, int R, bool kLong>
+__global__ __launch_bounds__(512) void paged_join_kernel(PagedArgs a, Work w) {
+    constexpr int kWaves = 8, kPer = D / 64;             // features lane, lane + 64 of a row
+    __shared__ float sm_m[kWaves], sm_l[kWaves], sm_o[kWaves][D];
+    const int id = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int r0 = kLong ? 16 * blockIdx.y : 0;
+    const Item it = w.items[id];
+    if (it.s < 0) return;
+    const Seq q = seq_of(a, it.s);
+    const int G = a.H / a.Hk;
+    const int rows = kLong ? min(min(R, q.n - it.row0), r0 + 16) : q.n * G;
+    const long long total = w.start[w.n], start = w.start[id];
+    const long long chunk = max((total + w.wgs - 1) / w.wgs, (long long)w.least);
+    const long long page0 = start + w.setup;
+    const int w0 = (int)(page0 / chunk), w1 = it.pages > 0 ? (int)((page0 + it.pages - 1) / chunk) : -1;
+    if (w0 == w1) return;                                // written already
+    const int parts = max(w1 - w0 + 1, 0);               // 0: no page
+    auto slot_of = [&](int p) {
+        const bool later = p == 0 && start > w0 * chunk;
+        return w.slots + (int64_t)(2 * (w0 + p) + later) * slot_floats<D>(R);
+    };
+    // rows by waves, or all waves on one row after the other, each with every eighth part
+    const int first = kLong ? 0 : wave, step = kLong ? 1 : kWaves;
+    const int mine = parts > first ? (parts - first + step - 1) / step : 0;
+    for (int r = kLong ? r0 + wave : 0; r < rows; r += kLong ? kWaves : 1) {
+        float M = -INFINITY, L = 0.f, o[kPer];
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
-    const float ref = M == -INFINITY ? 0.f : M;
-    const float w = fast_exp2(v.x - ref);
-    float L = v.y * w;
+        for (int k = 0; k < kPer; ++k) o[k] = 0.f;
+        // 64 parts at a time: a maximum and a sum per lane, then the rows, whose loads do not
+        // wait for each other
+        for (int p0 = 0; p0 < mine; p0 += 64) {
+            const int n = min(64, mine - p0);
+            float2 ml = make_float2(-INFINITY, 0.f);
+            if (lane < n) ml = *reinterpret_cast<const float2*>(slot_of(first + (p0 + lane) * step) + R * D + 2 * r);
+            float top = fmaxf(M, ml.x);
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) L += __shfl_xor(L, o);
-    float o0 = 0.f, o1 = 0.f;
-    for (int p = 0; p < splits; ++p) {
-        const float wp = __shfl(w, p);
-        if (__shfl(v.y, p) == 0.f) continue;            // (no key: its sums are not there)
-        o0 = __builtin_fmaf(wp, po[(int64_t)p * D + lane], o0);
-        if (D == 128) o1 = __builtin_fmaf(wp, po[(int64_t)p * D + 64 + lane], o1);
+            for (int i = 1; i < 64; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
+            const float ref = top == -INFINITY ? 0.f : top, x = fast_exp2(M - ref);
+            const float y = ml.y == 0.f ? 0.f : fast_exp2(ml.x - ref);   // (no key: its sums are zeros)
+            float l = ml.y == 0.f ? 0.f : ml.y * y;
+#pragma unroll
+            for (int i = 1; i < 64; i <<= 1) l += __shfl_xor(l, i);
+            M = top;
+            L = L * x + l;
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) o[k] *= x;
+#pragma unroll 8
+            for (int p = 0; p < n; ++p) {
+                const float* slot = slot_of(first + (p0 + p) * step) + r * D + lane;
+                const float yp = readlane_f32(y, p);
+#pragma unroll
+                for (int k = 0; k < kPer; ++k) o[k] = __builtin_fmaf(slot[64 * k], yp, o[k]);
+            }
+        }
+        if (!kLong) {
+            __syncthreads();                             // (the row before is written)
+            if (lane == 0) {
+                sm_m[wave] = M;
+                sm_l[wave] = L;
+            }
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) sm_o[wave][64 * k + lane] = o[k];
+            __syncthreads();
+            if (wave > 0) continue;
+            for (int v = 1; v < kWaves; ++v) {
+                const float mv = sm_m[v], lv = sm_l[v];
+                const float top = fmaxf(M, mv), ref = top == -INFINITY ? 0.f : top;
+                const float x = fast_exp2(M - ref), y = fast_exp2(mv - ref);
+                M = top;
+                L = L * x + lv * y;
+#pragma unroll
+                for (int k = 0; k < kPer; ++k) o[k] = o[k] * x + sm_o[v][64 * k + lane] * y;
+            }
+        }
+        const int h = kLong ? long_head(a, id, w.tiles) : id / w.tiles * G + r % G;
+        const int64_t row = (int64_t)(q.row0 + (kLong ? it.row0 + r : r / G)) * a.H + h;
+        const float inv = L == 0.f ? 0.f : 1.0f / L;
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) ((T*)a.O)[row * D + 64 * k + lane] = from_f32<T>(o[k] * inv);
+        if (lane == 0) a.lse[row] = L == 0.f ? -INFINITY : (M + fast_log2(L)) * kLn2;
     }
-    const float inv = L == 0.f ? 0.f : 1.0f / L;
-    ((T*)a.O)[row * D + lane] = from_f32<T>(o0 * inv);
-    if (D == 128) ((T*)a.O)[row * D + 64 + lane] = from_f32<T>(o1 * inv);
-    if (lane == 0) a.lse[row] = L == 0.f ? -INFINITY : (M + fast_log2(L)) * kLn2;
 }
 
 __global__ __launch_bounds__(256) void paged_flags_kernel(PagedArgs a, int limit) {
@@ -871,72 +1159,96 @@ __global__ __launch_bounds__(256) void paged_flags_kernel(PagedArgs a, int limit
 }
 
 // How a call is divided.  Sequences of at most short_max new tokens go to the short kernel,
-// the others to the long one.
+// the others to the long one, tiles of 64 nq rows.
 struct Division {
-    int short_max, nq;
+    int short_max, long_above, nq;
     bool short_on, long_on;
-    int tiles_short, tiles_long, split_short, split_long, stride;
+    Work lw, sw;       // offsets from the workspace in place of the pointers
+    size_t bytes;
 };
 
-// Parts of the keys: until `wgs` workgroups fill the chip three times, no part under `least`
-// pages of the longest sequence
-int parts(int64_t wgs, int64_t pages, int least) {
-    if (wgs <= 0) return 1;
-    int64_t p = (768 + wgs - 1) / wgs;
-    const int64_t most = pages / least;
-    if (p > most) p = most;
-    if (p > kMaxSplit) p = kMaxSplit;
-    return p < 1 ? 1 : (int)p;
+constexpr int kLeastShares = 96;
+constexpr int kSetup = 6;         // (less than any `least`)
+
+// A kernel's items, and their shares: `fit` workgroups (what the chip holds at a time), no
+// share under `least` pages.  Items that are many more, or have few pages, are not shared
+// out: at 8 items per workgroup the last ones to finish cost an eighth at most.
+void share_out(Work& w, int64_t items, int fit, int least, int64_t pages) {
+    w.n = (int)items;
+    w.least = least;
+    w.setup = kSetup;
+    w.shared = items < 8 * (int64_t)fit && pages > least;
+    int64_t wgs = items * pages / least + 1;
+    wgs = wgs < kLeastShares ? kLeastShares : wgs > fit ? fit : wgs;
+    w.wgs = w.shared ? (int)wgs : w.n;
 }
 
 Division divide(const PagedArgs& a) {
     Division v{};
-    const int G = a.H / a.Hk;
+    const int G = a.H / a.Hk, es = a.bf16 ? 2 : 4;
     v.short_max = kShortRows / G;
     const int64_t pages = (a.max_len + 63) / 64;
     v.long_on = a.max_new > v.short_max;
     // (rows in equal parts that are long: no sequence is short)
     v.short_on = !v.long_on || (int64_t)a.N * a.max_new != a.T;
+    v.long_above = v.short_on ? v.short_max : 0;
     v.nq = a.max_new > 64 ? 2 : 1;
     const int rows = 64 * v.nq;
-    // (no more tiles than this, however T rows are dealt to N sequences)
-    if (v.long_on) v.tiles_long = (int)((a.T + (int64_t)a.N * (rows - 1)) / rows);
-    v.tiles_short = v.short_on ? a.N : 0;
-    v.split_long = v.long_on ? parts((int64_t)v.tiles_long * a.H, pages, 4) : 1;
-    v.split_short = v.short_on ? parts((int64_t)v.tiles_short * a.Hk, pages, 8) : 1;
-    v.stride = v.split_long > v.split_short ? v.split_long : v.split_short;
+    auto take = [&](size_t n) {
+        const size_t at = v.bytes;
+        v.bytes += (n + 255) & ~(size_t)255;
+        return at;
+    };
+    auto place = [&](Work& w, int r) {
+        w.items = (Item*)take((size_t)w.n * sizeof(Item));
+        if (!w.shared) return;
+        w.start = (long long*)take((size_t)(w.n + 1) * sizeof(long long));
+        w.slots = (float*)take((size_t)2 * w.wgs * r * (a.d + 2) * sizeof(float));
+    };
+    if (v.long_on) {
+        // (no more tiles than this, however T rows are dealt to N sequences)
+        v.lw.tiles = (int)((a.T + (int64_t)a.N * (rows - 1)) / rows);
+        // workgroups at a time: by registers three per CU (d = 64, bfloat16) or by LDS two, one
+        const int fit = 256 * (a.d * es == 128 ? 3 : a.d * es == 256 ? 2 : 1);
+        share_out(v.lw, (int64_t)v.lw.tiles * a.H, fit, 8, pages);
+        place(v.lw, rows);
+    }
+    if (v.short_on) {
+        v.sw.tiles = a.N;
+        share_out(v.sw, (int64_t)a.N * a.Hk, a.d * es == 128 ? 512 : 256, 8, pages);
+        place(v.sw, kShortRows);
+    }
     return v;
 }
 
-template <typename T, int D>
+template <typename T, int D, int NQ>
 void attend(const PagedArgs& a, const Division& v, hipStream_t s) {
     const float kscale = kLog2e / sqrtf((float)D);
-    if (v.long_on) {
-        const dim3 grid(dealt((int64_t)v.tiles_long * v.split_long, a.H));
-        const int sm = v.short_on ? v.short_max : 0;
-        if (v.nq == 2)
-            hipLaunchKernelGGL((paged_long_kernel<T, D, 2>), grid, dim3(256), 0, s, a, v.tiles_long,
-                               v.split_long, v.stride, sm, kscale);
-        else
-            hipLaunchKernelGGL((paged_long_kernel<T, D, 1>), grid, dim3(256), 0, s, a, v.tiles_long,
-                               v.split_long, v.stride, sm, kscale);
+    Work lw = v.lw, sw = v.sw;
+    for (Work* w : {&lw, &sw}) {
+        w->items = (Item*)((char*)a.part + (size_t)w->items);
+        w->start = (long long*)((char*)a.part + (size_t)w->start);
+        w->slots = (float*)((char*)a.part + (size_t)w->slots);
     }
+    hipLaunchKernelGGL(paged_plan_kernel<64 * NQ>, dim3((lw.n + 7) / 8 + sw.n), dim3(512), 0, s, a, lw, sw,
+                       v.short_max, v.long_above);
+    if (v.long_on)
+        hipLaunchKernelGGL((paged_long_kernel<T, D, NQ>), dim3(lw.wgs), dim3(256), 0, s, a, lw, kscale);
     if (v.short_on)
-        hipLaunchKernelGGL((paged_short_kernel<T, D>),
-                           dim3(dealt((int64_t)v.tiles_short * v.split_short, a.Hk)), dim3(256), 0,
-                           s, a, v.split_short, v.stride, v.short_max, kscale);
-    if (v.stride > 1)
-        hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3((unsigned)(((int64_t)a.T * a.H + 3) / 4)), dim3(256),
-                           0, s, a, v.split_long, v.split_short, v.stride, v.short_on ? v.short_max : 0,
-                           v.long_on);
+        hipLaunchKernelGGL((paged_short_kernel<T, D>), dim3(sw.wgs), dim3(256), 0, s, a, sw, kscale);
+    if (lw.shared)
+        hipLaunchKernelGGL((paged_join_kernel<T, D, 64 * NQ, true>), dim3(lw.n, 4 * NQ), dim3(512), 0, s, a, lw);
+    if (sw.shared)
+        hipLaunchKernelGGL((paged_join_kernel<T, D, kShortRows, false>), dim3(sw.n), dim3(512), 0, s, a, sw);
+}
+template <typename T, int D>
+void attend(const PagedArgs& a, const Division& v, hipStream_t s) {
+    v.nq == 2 ? attend<T, D, 2>(a, v, s) : attend<T, D, 1>(a, v, s);
 }
 
 }  // namespace
 
-size_t paged_workspace(const PagedArgs& a) {
-    const Division v = divide(a);
-    return v.stride == 1 ? 0 : (size_t)a.T * a.H * v.stride * (a.d + 2) * sizeof(float);
-}
+size_t paged_workspace(const PagedArgs& a) { return divide(a).bytes; }
 
 hipError_t launch_paged_attend(const PagedArgs& a, hipStream_t s) {
     trace_begin(ACP_K_COUNT + ACP_OP_ATTEND, s);
