@@ -156,10 +156,6 @@ struct RowBlock {
     }
 };
 
-__device__ __forceinline__ float readlane_f32(float v, int l) {
-    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), l));
-}
-
 // Every lane's sum over the four lanes that hold a query
 __device__ __forceinline__ float over_groups(float v) {
     v += __shfl_xor(v, 16);
@@ -261,22 +257,31 @@ __device__ __forceinline__ int first_page(const PagedArgs& a, int s, int h, int 
 // ---- items and shares ------------------------------------------------------------------
 // An item: rows of a sequence that one head (short: one group of heads) takes over the pages
 // lo .. lo + pages - 1.
-struct Item {
+struct alignas(32) Item {
     int s;             // sequence, -1: no such item
-    int row0;          // first of its new rows
+    int t0, n;         // its first packed row, how many new tokens
+    int p0;            // position of the first
+    int len;           // of the sequence, its new rows included
     int lo, pages;
+    int pad;
+};
+// What a workgroup found at the start of its share: where the first page of it that another
+// share has pages in front of lies, for the merge (item -1: none, or an earlier share says so)
+struct alignas(16) Cut {
+    int item, skip, chunk, pad;
 };
 // The items of one kernel.  Item number (key head, tile, head of the group), in this order,
 // so that neighbouring shares read the same pages.
 struct Work {
     Item* items;
-    bool shared;       // in shares; else a workgroup per item
-    int setup;         // what taking up an item costs, in pages: its place in the list is that
-                       // much longer than its pages, in front of them
-    long long* start;  // [n + 1] where the items' places begin (written by workgroup 0)
+    int* places;       // [n] their lengths in the list (place_of)
+    Cut* cuts;         // [wgs]
     float* slots;      // [2 wgs] partial sums of a share's first item and of a later one
     int n, tiles;      // items; tiles of all sequences together, at most
     int wgs, least;    // workgroups; the least pages of a share
+    bool shared;       // in shares; else a workgroup per item
+    int setup;         // what taking up an item costs, in pages: its place in the list is that
+                       // much longer than its pages, in front of them
 };
 
 // Pages from lo up to those that the table has, for rows up to position last
@@ -303,32 +308,24 @@ __device__ __forceinline__ void report(const PagedArgs& a, int s, int h, int lan
     if (a.flags && lane == 0) atomicOr(a.flags + (int64_t)(s + late_zero()) * a.H + h, kFlagPage);
 }
 
-// The same in every lane, and known to be
-__device__ __forceinline__ Seq uniform_seq(const PagedArgs& a, int s) {
-    const Seq q = seq_of(a, s);
-    return Seq{__builtin_amdgcn_readfirstlane(q.row0), __builtin_amdgcn_readfirstlane(q.n),
-               __builtin_amdgcn_readfirstlane(q.past)};
-}
-
-// Long item `id` and its head, by a wave
+// Long item `id`, by a wave
 template <int kRows>
-__device__ __forceinline__ Item long_item(const PagedArgs& a, int id, int tiles, int short_max, int lane) {
-    const int G = a.H / a.Hk, hk = id / (tiles * G), rest = id - hk * tiles * G;
-    const int h = hk * G + rest % G;
-    Item it{-1, 0, 0, 0};
-    int tile;
+__device__ __forceinline__ Item long_item(const PagedArgs& a, int id, int tiles, int short_max, int h, int lane) {
+    const int G = a.H / a.Hk, rest = id - id / (tiles * G) * tiles * G;
+    Item it{-1, 0, 0, 0, 0, 0, 0, 0};
+    int s, tile;
     // (the last tiles of a sequence have the most pages: they go first)
-    if (!locate(a, tiles - 1 - rest / G, kRows, short_max, 0x7fffffff, lane, it.s, tile)) {
-        it.s = -1;
-        return it;
-    }
-    const Seq q = seq_of(a, it.s);
-    it.row0 = tile * kRows;
-    const int p0 = q.past + it.row0, p1 = p0 + min(kRows, q.n - it.row0) - 1;
-    it.lo = first_page(a, it.s, h, p0 >> 6, readfirst_f64(gate_at(a, it.s, h, p0)),
+    if (!locate(a, tiles - 1 - rest / G, kRows, short_max, 0x7fffffff, lane, s, tile)) return it;
+    const Seq q = seq_of(a, s);
+    it.s = s;
+    it.t0 = q.row0 + tile * kRows;
+    it.n = min(kRows, q.n - tile * kRows);
+    it.p0 = q.past + tile * kRows;
+    it.len = q.past + q.n;
+    it.lo = first_page(a, s, h, it.p0 >> 6, readfirst_f64(gate_at(a, s, h, it.p0)),
                        readfirst_f64(head_delta(a, h)), lane);
-    it.pages = page_count(a, it.lo, p1);
-    if ((p1 >> 6) >= a.W) report(a, it.s, h, lane);
+    it.pages = page_count(a, it.lo, it.p0 + it.n - 1);
+    if (((it.p0 + it.n - 1) >> 6) >= a.W) report(a, s, h, lane);
     return it;
 }
 __device__ __forceinline__ int long_head(const PagedArgs& a, int id, int tiles) {
@@ -336,54 +333,69 @@ __device__ __forceinline__ int long_head(const PagedArgs& a, int id, int tiles) 
     return hk * G + (id - hk * tiles * G) % G;
 }
 
-// Short item `id`, by kWaves waves: the first page that any head of the group keeps for the
-// first token
-template <int kWaves>
-__device__ __forceinline__ Item short_item(const PagedArgs& a, int id, int tiles, int short_max, int wave,
-                                           int lane, int (&first)[16]) {
-    const int G = a.H / a.Hk, hk = id / tiles;
-    Item it{-1, 0, 0, 0};
-    int tile;
-    if (!locate(a, id - hk * tiles, short_max, 0, short_max, lane, it.s, tile)) {
-        it.s = -1;
-        return it;                                   // (every wave alike)
-    }
-    const Seq q = seq_of(a, it.s);
-    const int last = q.past + q.n - 1;
-    for (int k = wave; k < G; k += kWaves) {
-        const int h = hk * G + k;
-        const int f = first_page(a, it.s, h, q.past >> 6, readfirst_f64(gate_at(a, it.s, h, q.past)),
-                                 readfirst_f64(head_delta(a, h)), lane);
-        if (lane == 0) first[k] = f;
-        if ((last >> 6) >= a.W) report(a, it.s, h, lane);
-    }
-    __syncthreads();
-    it.lo = first[0];
-    for (int k = 1; k < G; ++k) it.lo = min(it.lo, first[k]);
-    it.pages = page_count(a, it.lo, last);
-    return it;
+__device__ __forceinline__ int place_of(const Work& w, int pages) { return pages > 0 ? pages + w.setup : 0; }
+
+// Rows without a page: O = 0, lse = -inf (lane: feature)
+template <typename T>
+__device__ __forceinline__ void empty_row(const PagedArgs& a, int t, int h, int lane) {
+    const int64_t row = (int64_t)t * a.H + h;
+    for (int f = lane; f < a.d; f += 64) ((T*)a.O)[row * a.d + f] = from_f32<T>(0.f);
+    if (lane == 0) a.lse[row] = -INFINITY;
 }
 
-// The items of both kernels: 8 long ones, or a short one, per workgroup of 8 waves
-template <int kRows>
+// The items of both kernels, by workgroups of 8 waves: a wave per long item, and per head of
+// a short one (8 of them at a time), whose first page is the first that any head of the group
+// keeps for the first token.
+template <typename T, int kRows>
 __global__ __launch_bounds__(512) void paged_plan_kernel(PagedArgs a, Work lw, Work sw, int short_max,
-                                                         int long_above) {
-    __shared__ int first[16];
+                                                         int long_above, int short_waves) {
+    __shared__ int first[8][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int nl = (lw.n + 7) / 8;
+    const int nl = (lw.n + 7) / 8, G = a.H / a.Hk;
     if ((int)blockIdx.x < nl) {
         const int id = blockIdx.x * 8 + wave;
         if (id >= lw.n) return;
-        const Item it = long_item<kRows>(a, id, lw.tiles, long_above, lane);
-        if (lane == 0) lw.items[id] = it;
-    } else {
-        const int id = blockIdx.x - nl;
-        const Item it = short_item<8>(a, id, sw.tiles, short_max, wave, lane, first);
-        if (threadIdx.x == 0) sw.items[id] = it;
+        const int h = long_head(a, id, lw.tiles);
+        const Item it = long_item<kRows>(a, id, lw.tiles, long_above, h, lane);
+        if (lane == 0) {
+            lw.items[id] = it;
+            lw.places[id] = place_of(lw, it.pages);
+        }
+        if (it.s >= 0 && it.pages == 0)
+            for (int r = 0; r < it.n; ++r) empty_row<T>(a, it.t0 + r, h, lane);
+        return;
+    }
+    const int slot = wave / short_waves, w = wave - slot * short_waves;
+    const int id = (blockIdx.x - nl) * (8 / short_waves) + slot;
+    const int hk = min(id / sw.tiles, a.Hk - 1);
+    Item it{-1, 0, 0, 0, 0, 0, 0, 0};
+    int s, tile;
+    if (id < sw.n && locate(a, id - hk * sw.tiles, short_max, 0, short_max, lane, s, tile)) {
+        const Seq q = seq_of(a, s);
+        it = Item{s, q.row0, q.n, q.past, q.past + q.n, 0, 0, 0};
+        for (int k = w; k < G; k += short_waves) {
+            const int h = hk * G + k;
+            const int f = first_page(a, s, h, q.past >> 6, readfirst_f64(gate_at(a, s, h, q.past)),
+                                     readfirst_f64(head_delta(a, h)), lane);
+            if (lane == 0) first[slot][k] = f;
+            if (((it.len - 1) >> 6) >= a.W) report(a, s, h, lane);
+        }
+    }
+    __syncthreads();
+    if (id >= sw.n || w > 0) return;
+    if (it.s >= 0) {
+        it.lo = first[slot][0];
+        for (int k = 1; k < G; ++k) it.lo = min(it.lo, first[slot][k]);
+        it.pages = page_count(a, it.lo, it.len - 1);
+        if (it.pages == 0)
+            for (int r = 0; r < it.n * G; ++r) empty_row<T>(a, it.t0 + r / G, hk * G + r % G, lane);
+    }
+    if (lane == 0) {
+        sw.items[id] = it;
+        sw.places[id] = place_of(sw, it.pages);
     }
 }
 
-__device__ __forceinline__ int place_of(const Work& w, int pages) { return pages > 0 ? pages + w.setup : 0; }
 
 // A workgroup's share: `left` of the list from `skip` in item `item`'s place on
 struct Share {
@@ -394,15 +406,14 @@ struct ShareSmem {
     long long wave[4];
     int item, skip, left;
 };
-// The share of workgroup wg (256 threads); left = 0: none.  Workgroup 0 also writes the list
-// of starts for the merge.  A share fits an int: fewer than 8 items per workgroup are shared
-// out, to at least kLeastShares, of at most 2^25 pages each.
+// The share of workgroup wg (256 threads); left = 0: none.  A share fits an int: fewer than 8
+// items per workgroup are shared out, to at least kLeastShares, of at most 2^25 pages each.
 __device__ __forceinline__ Share find_share(const Work& w, int wg, ShareSmem& sm) {
     if (!w.shared) return Share{wg, 0, 0x7fffffff, false};        // the item, whole
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     const int per = (w.n + 255) / 256, i0 = min(t * per, w.n), i1 = min(i0 + per, w.n);
     long long sum = 0;
-    for (int i = i0; i < i1; ++i) sum += place_of(w, w.items[i].pages);
+    for (int i = i0; i < i1; ++i) sum += w.places[i];
     long long incl = sum;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -419,22 +430,18 @@ __device__ __forceinline__ Share find_share(const Work& w, int wg, ShareSmem& sm
         total += sm.wave[k];
     }
     long long before = incl - sum;
-    if (wg == 0) {
-        long long b = before;
-        for (int i = i0; i < i1; ++i) {
-            w.start[i] = b;
-            b += place_of(w, w.items[i].pages);
-        }
-        if (t == 255) w.start[w.n] = total;
-    }
     const long long chunk = max((total + w.wgs - 1) / w.wgs, (long long)w.least), at = wg * chunk;
     if (at < total && before <= at && at < incl) {       // (one thread: its items hold pages)
         int i = i0;
-        for (; before + place_of(w, w.items[i].pages) <= at; ++i) before += place_of(w, w.items[i].pages);
+        for (; before + w.places[i] <= at; ++i) before += w.places[i];
+        const int skip = (int)(at - before);
         sm.item = i;
-        sm.skip = (int)(at - before);
+        sm.skip = skip;
         sm.left = (int)min(chunk, total - at);
+        const bool mine = skip > w.setup && skip - chunk <= w.setup;
+        w.cuts[wg] = Cut{mine ? i : -1, skip, (int)chunk, 0};
     }
+    if (at >= total && t == 0) w.cuts[wg] = Cut{-1, 0, 0, 0};
     __syncthreads();
     return Share{__builtin_amdgcn_readfirstlane(sm.item), __builtin_amdgcn_readfirstlane(sm.skip),
                  __builtin_amdgcn_readfirstlane(sm.left), false};
@@ -452,13 +459,13 @@ __device__ __forceinline__ bool next_item(const Work& w, Share& sh, const Item& 
     sh.skip = 0;
     sh.later = true;
     do ++sh.item;
-    while (__builtin_amdgcn_readfirstlane(w.items[sh.item].pages) == 0);
+    while (__builtin_amdgcn_readfirstlane(w.places[sh.item]) == 0);
     return true;
 }
 __device__ __forceinline__ Item item_at(const Work& w, int i) {
     const Item t = w.items[i];
-    return Item{__builtin_amdgcn_readfirstlane(t.s), __builtin_amdgcn_readfirstlane(t.row0),
-                __builtin_amdgcn_readfirstlane(t.lo), __builtin_amdgcn_readfirstlane(t.pages)};
+    auto u = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    return Item{u(t.s), u(t.t0), u(t.n), u(t.p0), u(t.len), u(t.lo), u(t.pages), 0};
 }
 
 // Page numbers of 64 consecutive pages, one per lane
@@ -598,18 +605,15 @@ void paged_long_kernel(PagedArgs, Work work, float kscale) {
     const int lane = tid & 63, g = lane >> 4, r16 = lane & 15;
     const PagedArgs& a = late_args();
     const Item it = item_at(work, sh.item);
-    if (it.s < 0) return;                               // (not in a share)
-    const int s = it.s, row0 = it.row0, h = long_head(a, sh.item, work.tiles);
+    if (it.pages == 0) return;                          // (not in a share)
+    const int s = it.s, h = long_head(a, sh.item, work.tiles);
     // this share's pages of the item
     int nb;
     const int taken = pages_here(work, sh, it, nb), ne = nb + taken - 1;
     if (work.shared && taken == 0) return;
-    const Seq q = uniform_seq(a, s);
     const int hk = h / (a.H / a.Hk);
     const double delta = readfirst_f64(head_delta(a, h));
-    const int rows = min(kRows, q.n - row0);                         // of the sequence's new rows
-    const int p0 = q.past + row0, p1 = p0 + rows - 1;                // positions of the tile
-    const int len = q.past + q.n;
+    const int rows = it.n, p0 = it.p0, p1 = p0 + rows - 1, len = it.len;
 
     auto gate = [&](int pos) __attribute__((always_inline)) { return gate_at(a, s, h, pos); };
     const double R = readfirst_f64(gate(p0));
@@ -627,7 +631,7 @@ void paged_long_kernel(PagedArgs, Work work, float kscale) {
     for (int qt = 0; qt < NQ; ++qt) {
         const int pos = pos_of(qt), i = o0 + 16 * qt + r16;
         const double ci = gate(pos), r = ci - R;
-        blk.load_q(qt, (const T*)a.q + (int64_t)(q.row0 + pos - q.past) * a.qt + (int64_t)h * a.qh, g);
+        blk.load_q(qt, (const T*)a.q + (int64_t)(it.t0 + pos - p0) * a.qt + (int64_t)h * a.qh, g);
         // (the wave's own rows: no other reads them)
         const float hi = (float)r;
         sm.rc[i] = ci;
@@ -823,7 +827,7 @@ void paged_long_kernel(PagedArgs, Work work, float kscale) {
             const int r = o0 + 16 * qt + r16;
             if (r >= rows) continue;
             if (nb <= ne && sm.marked) add_marks<D>(blk.acc[qt], sm.inf[r], g);
-            if (taken == it.pages) put_row<T, D>(a, q.row0 + row0 + r, h, blk.acc[qt], blk.max_logit(qt), l, g);
+            if (taken == it.pages) put_row<T, D>(a, it.t0 + r, h, blk.acc[qt], blk.max_logit(qt), l, g);
             else put_part<D, kRows>(slot, r, blk.acc[qt], blk.max_logit(qt), l, g);
         }
     }
@@ -862,23 +866,21 @@ __global__ __launch_bounds__(256) void paged_short_kernel(PagedArgs, Work work, 
     asm volatile("" : "+v"(tid));
     const int lane = tid & 63, g = lane >> 4, r16 = lane & 15;
     const Item it = item_at(work, sh.item);
-    if (it.s < 0) return;                               // (not in a share)
+    if (it.pages == 0) return;                          // (not in a share)
     const int s = it.s, hk = sh.item / work.tiles;
     int nb;
     const int taken = pages_here(work, sh, it, nb), ne = nb + taken - 1;
     if (work.shared && taken == 0) return;
-    const Seq q = uniform_seq(a, s);
-    const int G = a.H / a.Hk, nrows = q.n * G;
-    const int len = q.past + q.n;
+    const int G = a.H / a.Hk, nrows = it.n * G, len = it.len;
     // the lane's row (those past the end repeat the last one)
     const int r = min(r16, nrows - 1);
-    const int h = hk * G + r % G, pi = q.past + r / G;
+    const int h = hk * G + r % G, pi = it.p0 + r / G;
     const int pp = page_of(a, s, pi >> 6);
     const double ci = pp < 0 ? 0.0 : gates_of(a, pp, h)[pi & 63];
     const double delta = head_delta(a, h);
     Block blk;
     blk.clear();
-    blk.load_q(0, (const T*)a.q + (int64_t)(q.row0 + r / G) * a.qt + (int64_t)h * a.qh, g);
+    blk.load_q(0, (const T*)a.q + (int64_t)(it.t0 + r / G) * a.qt + (int64_t)h * a.qh, g);
 
     if (tid == 0) sm.marked = 0;
     for (int i = tid; i < 16 * 2 * (D / 32); i += 256) (&sm.inf[0][0][0])[i] = 0;
@@ -1049,7 +1051,7 @@ __global__ __launch_bounds__(256) void paged_short_kernel(PagedArgs, Work work, 
         }
         if (sm.marked) add_marks<D>(blk.acc[0], sm.inf[r16], g);
         if (r16 < nrows) {
-            if (taken == it.pages) put_row<T, D>(a, q.row0 + r / G, h, blk.acc[0], M, L, g);
+            if (taken == it.pages) put_row<T, D>(a, it.t0 + r / G, h, blk.acc[0], M, L, g);
             else put_part<D, 16>(work.slots + (int64_t)(2 * wg + sh.later) * slot_floats<D>(16), r16,
                                  blk.acc[0], M, L, g);
         }
@@ -1060,90 +1062,94 @@ __global__ __launch_bounds__(256) void paged_short_kernel(PagedArgs, Work work, 
 }
 
 // ---- merge -----------------------------------------------------------------------------
-// The partial sums of an item that lies in several shares, of R rows per slot; an item
-// without a page gets O = 0, lse = -inf.  A workgroup per item, the parts dealt to its waves
-// (kLong: per 16 rows, these dealt to them).
+// The partial sums of an item that lies in several shares, of R rows per slot.  A workgroup
+// per share, for the item whose first cut lies at the share's start, and per 16 rows: 16 lanes
+// take a row (four rows of a slot in one load of a wave), or, of fewer rows, every so many
+// lanes' parts of it.
 template <typename T, int D, int R, bool kLong>
-__global__ __launch_bounds__(512) void paged_join_kernel(PagedArgs a, Work w) {
-    constexpr int kWaves = 8, kPer = D / 64;             // features lane, lane + 64 of a row
-    __shared__ float sm_m[kWaves], sm_l[kWaves], sm_o[kWaves][D];
-    const int id = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int r0 = kLong ? 16 * blockIdx.y : 0;
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a, Work w) {
+    constexpr int kPer = D / 64;                         // features 64 k + 4 l .. + 3 of lane l
+    __shared__ float sm[16][D + 2];
+    const int wg = blockIdx.x + 1;
+    const Cut cut = w.cuts[wg];
+    if (cut.item < 0) return;
+    const int id = cut.item;
     const Item it = w.items[id];
-    if (it.s < 0) return;
-    const Seq q = seq_of(a, it.s);
-    const int G = a.H / a.Hk;
-    const int rows = kLong ? min(min(R, q.n - it.row0), r0 + 16) : q.n * G;
-    const long long total = w.start[w.n], start = w.start[id];
-    const long long chunk = max((total + w.wgs - 1) / w.wgs, (long long)w.least);
-    const long long page0 = start + w.setup;
-    const int w0 = (int)(page0 / chunk), w1 = it.pages > 0 ? (int)((page0 + it.pages - 1) / chunk) : -1;
-    if (w0 == w1) return;                                // written already
-    const int parts = max(w1 - w0 + 1, 0);               // 0: no page
-    auto slot_of = [&](int p) {
-        const bool later = p == 0 && start > w0 * chunk;
-        return w.slots + (int64_t)(2 * (w0 + p) + later) * slot_floats<D>(R);
+    const int G = a.H / a.Hk, r0 = 16 * blockIdx.y;
+    const int rows = min(16, (kLong ? it.n : it.n * G) - r0);
+    if (rows <= 0) return;
+    // the share before has its first pages; its last one lies here or in a later share
+    const int w0 = wg - 1, parts = 2 + (w.setup - cut.skip + it.pages - 1) / cut.chunk;
+    const int group = threadIdx.x >> 4, l16 = threadIdx.x & 15;
+    const int each = rows == 1 ? 16 : rows == 2 ? 8 : rows <= 4 ? 4 : rows <= 8 ? 2 : 1;   // groups per row
+    const int r = r0 + group / each, first = group % each;
+    const bool on = group / each < rows;
+    float M = -INFINITY, L = 0.f;
+    f32x4 o[kPer];
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) o[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // (a part without a key of the row has zeros and the weight 0)
+    auto merge = [&](float m, float l, const f32x4 (&v)[kPer]) __attribute__((always_inline)) {
+        const float top = fmaxf(M, m), ref = top == -INFINITY ? 0.f : top;
+        const float x = fast_exp2(M - ref), y = fast_exp2(m - ref);
+        M = top;
+        L = L * x + l * y;
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) o[k] = o[k] * x + v[k] * y;
     };
-    // rows by waves, or all waves on one row after the other, each with every eighth part
-    const int first = kLong ? 0 : wave, step = kLong ? 1 : kWaves;
-    const int mine = parts > first ? (parts - first + step - 1) / step : 0;
-    for (int r = kLong ? r0 + wave : 0; r < rows; r += kLong ? kWaves : 1) {
-        float M = -INFINITY, L = 0.f, o[kPer];
+    if (on) {
+        constexpr int kAtOnce = 4;
+        for (int p = first; p < parts; p += kAtOnce * each) {
+            float2 ml[kAtOnce];
+            f32x4 v[kAtOnce][kPer];
 #pragma unroll
-        for (int k = 0; k < kPer; ++k) o[k] = 0.f;
-        // 64 parts at a time: a maximum and a sum per lane, then the rows, whose loads do not
-        // wait for each other
-        for (int p0 = 0; p0 < mine; p0 += 64) {
-            const int n = min(64, mine - p0);
-            float2 ml = make_float2(-INFINITY, 0.f);
-            if (lane < n) ml = *reinterpret_cast<const float2*>(slot_of(first + (p0 + lane) * step) + R * D + 2 * r);
-            float top = fmaxf(M, ml.x);
+            for (int i = 0; i < kAtOnce; ++i) {
+                const int q = min(p + i * each, parts - 1);
+                const bool later = q == 0 && cut.skip < cut.chunk;
+                const float* slot = w.slots + (int64_t)(2 * (w0 + q) + later) * slot_floats<D>(R);
+                ml[i] = *reinterpret_cast<const float2*>(slot + R * D + 2 * r);
 #pragma unroll
-            for (int i = 1; i < 64; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
-            const float ref = top == -INFINITY ? 0.f : top, x = fast_exp2(M - ref);
-            const float y = ml.y == 0.f ? 0.f : fast_exp2(ml.x - ref);   // (no key: its sums are zeros)
-            float l = ml.y == 0.f ? 0.f : ml.y * y;
-#pragma unroll
-            for (int i = 1; i < 64; i <<= 1) l += __shfl_xor(l, i);
-            M = top;
-            L = L * x + l;
-#pragma unroll
-            for (int k = 0; k < kPer; ++k) o[k] *= x;
-#pragma unroll 8
-            for (int p = 0; p < n; ++p) {
-                const float* slot = slot_of(first + (p0 + p) * step) + r * D + lane;
-                const float yp = readlane_f32(y, p);
-#pragma unroll
-                for (int k = 0; k < kPer; ++k) o[k] = __builtin_fmaf(slot[64 * k], yp, o[k]);
+                for (int k = 0; k < kPer; ++k)
+                    v[i][k] = *reinterpret_cast<const f32x4*>(slot + r * D + 64 * k + 4 * l16);
             }
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i)
+                if (p + i * each < parts) merge(ml[i].x, ml[i].y, v[i]);
         }
-        if (!kLong) {
-            __syncthreads();                             // (the row before is written)
-            if (lane == 0) {
-                sm_m[wave] = M;
-                sm_l[wave] = L;
-            }
-#pragma unroll
-            for (int k = 0; k < kPer; ++k) sm_o[wave][64 * k + lane] = o[k];
-            __syncthreads();
-            if (wave > 0) continue;
-            for (int v = 1; v < kWaves; ++v) {
-                const float mv = sm_m[v], lv = sm_l[v];
-                const float top = fmaxf(M, mv), ref = top == -INFINITY ? 0.f : top;
-                const float x = fast_exp2(M - ref), y = fast_exp2(mv - ref);
-                M = top;
-                L = L * x + lv * y;
-#pragma unroll
-                for (int k = 0; k < kPer; ++k) o[k] = o[k] * x + sm_o[v][64 * k + lane] * y;
-            }
-        }
-        const int h = kLong ? long_head(a, id, w.tiles) : id / w.tiles * G + r % G;
-        const int64_t row = (int64_t)(q.row0 + (kLong ? it.row0 + r : r / G)) * a.H + h;
-        const float inv = L == 0.f ? 0.f : 1.0f / L;
-#pragma unroll
-        for (int k = 0; k < kPer; ++k) ((T*)a.O)[row * D + 64 * k + lane] = from_f32<T>(o[k] * inv);
-        if (lane == 0) a.lse[row] = L == 0.f ? -INFINITY : (M + fast_log2(L)) * kLn2;
     }
+    if (each > 1) {
+#pragma unroll
+        for (int k = 0; k < kPer; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sm[group][64 * k + 4 * l16 + e] = o[k][e];
+        if (l16 == 0) {
+            sm[group][D] = M;
+            sm[group][D + 1] = L;
+        }
+        __syncthreads();
+        if (first > 0) return;
+        for (int i = 1; i < each; ++i) {
+            const float* q = sm[group + i];
+            f32x4 v[kPer];
+#pragma unroll
+            for (int k = 0; k < kPer; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[k][e] = q[64 * k + 4 * l16 + e];
+            merge(q[D], q[D + 1], v);
+        }
+    }
+    if (!on) return;
+    const int h = kLong ? long_head(a, id, w.tiles) : id / w.tiles * G + r % G;
+    const int64_t row = (int64_t)(it.t0 + (kLong ? r : r / G)) * a.H + h;
+    const float inv = L == 0.f ? 0.f : 1.0f / L;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        T out[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[e] = from_f32<T>(o[k][e] * inv);
+        __builtin_memcpy((T*)a.O + row * D + 64 * k + 4 * l16, out, sizeof(out));
+    }
+    if (l16 == 0) a.lse[row] = L == 0.f ? -INFINITY : (M + fast_log2(L)) * kLn2;
 }
 
 __global__ __launch_bounds__(256) void paged_flags_kernel(PagedArgs a, int limit) {
@@ -1201,8 +1207,9 @@ Division divide(const PagedArgs& a) {
     };
     auto place = [&](Work& w, int r) {
         w.items = (Item*)take((size_t)w.n * sizeof(Item));
+        w.places = (int*)take((size_t)w.n * sizeof(int));
         if (!w.shared) return;
-        w.start = (long long*)take((size_t)(w.n + 1) * sizeof(long long));
+        w.cuts = (Cut*)take((size_t)w.wgs * sizeof(Cut));
         w.slots = (float*)take((size_t)2 * w.wgs * r * (a.d + 2) * sizeof(float));
     };
     if (v.long_on) {
@@ -1227,19 +1234,22 @@ void attend(const PagedArgs& a, const Division& v, hipStream_t s) {
     Work lw = v.lw, sw = v.sw;
     for (Work* w : {&lw, &sw}) {
         w->items = (Item*)((char*)a.part + (size_t)w->items);
-        w->start = (long long*)((char*)a.part + (size_t)w->start);
+        w->places = (int*)((char*)a.part + (size_t)w->places);
+        w->cuts = (Cut*)((char*)a.part + (size_t)w->cuts);
         w->slots = (float*)((char*)a.part + (size_t)w->slots);
     }
-    hipLaunchKernelGGL(paged_plan_kernel<64 * NQ>, dim3((lw.n + 7) / 8 + sw.n), dim3(512), 0, s, a, lw, sw,
-                       v.short_max, v.long_above);
+    const int G = a.H / a.Hk, waves = G <= 1 ? 1 : G <= 2 ? 2 : G <= 4 ? 4 : 8;   // of a short item
+    hipLaunchKernelGGL((paged_plan_kernel<T, 64 * NQ>), dim3((lw.n + 7) / 8 + (sw.n * waves + 7) / 8), dim3(512), 0,
+                       s, a, lw, sw, v.short_max, v.long_above, waves);
     if (v.long_on)
         hipLaunchKernelGGL((paged_long_kernel<T, D, NQ>), dim3(lw.wgs), dim3(256), 0, s, a, lw, kscale);
     if (v.short_on)
         hipLaunchKernelGGL((paged_short_kernel<T, D>), dim3(sw.wgs), dim3(256), 0, s, a, sw, kscale);
     if (lw.shared)
-        hipLaunchKernelGGL((paged_join_kernel<T, D, 64 * NQ, true>), dim3(lw.n, 4 * NQ), dim3(512), 0, s, a, lw);
+        hipLaunchKernelGGL((paged_join_kernel<T, D, 64 * NQ, true>), dim3(lw.wgs - 1, 4 * NQ), dim3(256), 0, s, a,
+                           lw);
     if (sw.shared)
-        hipLaunchKernelGGL((paged_join_kernel<T, D, kShortRows, false>), dim3(sw.n), dim3(512), 0, s, a, sw);
+        hipLaunchKernelGGL((paged_join_kernel<T, D, kShortRows, false>), dim3(sw.wgs - 1), dim3(256), 0, s, a, sw);
 }
 template <typename T, int D>
 void attend(const PagedArgs& a, const Division& v, hipStream_t s) {
