@@ -1174,15 +1174,14 @@ struct Division {
 };
 
 constexpr int kLeastShares = 96;
-constexpr int kSetup = 6;         // (less than any `least`)
 
 // A kernel's items, and their shares: `fit` workgroups (what the chip holds at a time), no
 // share under `least` pages.  Items that are many more, or have few pages, are not shared
 // out: at 8 items per workgroup the last ones to finish cost an eighth at most.
-void share_out(Work& w, int64_t items, int fit, int least, int64_t pages) {
+void share_out(Work& w, int64_t items, int fit, int setup, int least, int64_t pages) {
     w.n = (int)items;
     w.least = least;
-    w.setup = kSetup;
+    w.setup = setup;
     w.shared = items < 8 * (int64_t)fit && pages > least;
     int64_t wgs = items * pages / least + 1;
     wgs = wgs < kLeastShares ? kLeastShares : wgs > fit ? fit : wgs;
@@ -1217,12 +1216,12 @@ Division divide(const PagedArgs& a) {
         v.lw.tiles = (int)((a.T + (int64_t)a.N * (rows - 1)) / rows);
         // workgroups at a time: by registers three per CU (d = 64, bfloat16) or by LDS two, one
         const int fit = 256 * (a.d * es == 128 ? 3 : a.d * es == 256 ? 2 : 1);
-        share_out(v.lw, (int64_t)v.lw.tiles * a.H, fit, 8, pages);
+        share_out(v.lw, (int64_t)v.lw.tiles * a.H, fit, a.bf16 ? 9 : 2, a.bf16 ? 10 : 4, pages);
         place(v.lw, rows);
     }
     if (v.short_on) {
         v.sw.tiles = a.N;
-        share_out(v.sw, (int64_t)a.N * a.Hk, a.d * es == 128 ? 512 : 256, 8, pages);
+        share_out(v.sw, (int64_t)a.N * a.Hk, a.bf16 ? 512 : 256, 7, 8, pages);
         place(v.sw, kShortRows);
     }
     return v;

@@ -94,28 +94,37 @@ def acp_op_timing_read() -> dict:
 # ---- marshalling -----------------------------------------------------------------------
 
 def _device(*ts):
-    dev = ts[0].device
+    """The device of all of them, by index (cheaper than device objects)."""
+    d = ts[0].get_device()
     for t in ts:
-        if t.device.type != "cuda":
-            raise ValueError("tensors must live on the GPU")
-        if t.device != dev:
+        if t.get_device() != d:
             raise ValueError("tensors must live on one GPU")
-    return dev
+    if d < 0:
+        raise ValueError("tensors must live on the GPU")
+    return d
 
 
-def _run(fn, dev, *args):
-    """fn(*args, stream) on `dev`'s current stream."""
-    if dev.index == torch.cuda.current_device():
-        status = fn(*args, acp._stream(dev))
+def _stream(d: int) -> int:
+    if acp._raw_stream is not None:
+        return acp._raw_stream(d)
+    return torch.cuda.current_stream(d).cuda_stream
+
+
+def _run(fn, d, *args):
+    """fn(*args, stream) on the current stream of device d."""
+    if d == torch.cuda.current_device():
+        status = fn(*args, _stream(d))
     else:
-        with torch.cuda.device(dev):
-            status = fn(*args, acp._stream(dev))
+        with torch.cuda.device(d):
+            status = fn(*args, _stream(d))
     if status != acp.ACP_OK:
         acp._check(status)
 
 
 def _strides(t: torch.Tensor):
-    """Element strides of the three leading axes of a 4-D tensor."""
+    """Element strides of the three leading axes of a 4-D tensor (None: contiguous)."""
+    if t.is_contiguous():
+        return None
     s = t.stride()
     return (_i64 * 3)(s[0], s[1], s[2])
 
@@ -163,12 +172,12 @@ def norm_forward(x, weight, bias=None, eps: float = 1e-6, center: bool = False, 
     if not weight.is_contiguous() or (bias is not None and not bias.is_contiguous()):
         raise ValueError("weight and bias must be contiguous")
     B, H, L, n = x4.shape
-    y = torch.empty(x.shape, dtype=x.dtype, device=dev) if out is None else out
+    y = x.new_empty(x.shape) if out is None else out
     if out is not None and (out.shape != x.shape or out.dtype != x.dtype or not out.is_contiguous()
-                            or out.device != dev):
+                            or out.get_device() != dev):
         raise ValueError("out must be contiguous and like x")
-    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=dev) if stats and center else None
-    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=dev) if stats else None
+    mean = x.new_empty(x.shape[:-1], dtype=torch.float32) if stats and center else None
+    rstd = x.new_empty(x.shape[:-1], dtype=torch.float32) if stats else None
     _run(lib().acp_norm_fwd, dev, x4.data_ptr(), _strides(x4), weight.data_ptr(), _ptr(bias), acp._dt(x),
          acp._dt(weight), B, H, L, n, per_head, center, eps, y.data_ptr(), _ptr(mean), _ptr(rstd))
     return y, mean, rstd
@@ -182,7 +191,7 @@ def norm_backward(dy, x, weight, mean, rstd, bias: bool = False):
         raise ValueError("dy must match x")
     for name, t in (("mean", mean), ("rstd", rstd)):
         if t is not None and (t.shape != x.shape[:-1] or t.dtype != torch.float32
-                              or not t.is_contiguous() or t.device != dev):
+                              or not t.is_contiguous() or t.get_device() != dev):
             raise ValueError(name + " must be norm_forward's")
     if not weight.is_contiguous():
         raise ValueError("weight must be contiguous")
@@ -193,14 +202,14 @@ def norm_backward(dy, x, weight, mean, rstd, bias: bool = False):
     B, H, L, n = x4.shape
     dy4 = dy4.view(x4.shape) if dy4.dim() != 4 else dy4
     dx4 = torch.empty_like(x4)
-    dw = torch.empty(weight.shape, dtype=torch.float32, device=dev)
+    dw = x.new_empty(weight.shape, dtype=torch.float32)
     db = torch.empty_like(dw) if bias else None
     need = _sz(0)
     acp._check(lib().acp_norm_workspace_size(B, H, L, n, per_head, ctypes.byref(need)))
-    ws = torch.empty(max(need.value, 16), dtype=torch.uint8, device=dev)
+    ws = dw.new_empty(need.value // 4 + 4)
     _run(lib().acp_norm_bwd, dev, dy4.data_ptr(), _strides(dy4), x4.data_ptr(), _strides(x4),
          weight.data_ptr(), acp._dt(x), acp._dt(weight), B, H, L, n, per_head, _ptr(mean), rstd.data_ptr(),
-         dx4.data_ptr(), _strides(dx4), dw.data_ptr(), _ptr(db), ws.data_ptr(), ws.numel())
+         dx4.data_ptr(), _strides(dx4), dw.data_ptr(), _ptr(db), ws.data_ptr(), 4 * ws.numel())
     return dx4.view(x.shape) if dx4.shape != x.shape else dx4, dw, db
 
 
@@ -276,19 +285,18 @@ class Rotary:
                                                or k.shape[2:] != q.shape[2:] or k.dtype != q.dtype)):
             raise ValueError("q must be [B, H, L, d] and k [B, Hk, L, d] of its type")
         B, H, L, d = q.shape
-        ins = (q, k)
         if out is None:
-            out = tuple(None if t is None else torch.empty(t.shape, dtype=t.dtype, device=dev) for t in ins)
-        for t, o in zip(ins, out):
+            out = (q.new_empty(q.shape), None if k is None else k.new_empty(k.shape))
+        for t, o in zip((q, k), out):
             if t is None:
                 continue
             if t.stride(3) != 1 or o.stride(3) != 1:
                 raise ValueError("features must be contiguous")
-            if o.shape != t.shape or o.dtype != t.dtype or o.device != dev:
+            if o.shape != t.shape or o.dtype != t.dtype or o.get_device() != dev:
                 raise ValueError("out must be like its input")
         pos = None
         if positions is not None:
-            if positions.dtype not in (torch.int32, torch.int64) or positions.device != dev:
+            if positions.dtype not in (torch.int32, torch.int64) or positions.get_device() != dev:
                 raise ValueError("positions must be int32 or int64 on the tensors' GPU")
             if tuple(positions.shape) == (L,):
                 pos = (_i64 * 2)(0, positions.stride(0))
@@ -370,6 +378,8 @@ class PagedCache:
         if t.stride(2) != 1:
             raise ValueError(name + ": features must be contiguous")
         # (an axis of one has any stride)
+        if t.is_contiguous():
+            return None
         return (_i64 * 2)(t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if heads > 1 else 0)
 
     def append(self, k, v, log_f, cu, past, table, flags=None):
@@ -382,7 +392,7 @@ class PagedCache:
         if v.shape[0] != T or log_f.shape != (T, self.H) or log_f.dtype != torch.float32:
             raise ValueError("v must be like k, and log_f float32 [T, H]")
         _run(lib().acp_paged_append, dev, k.data_ptr(), ks, v.data_ptr(), vs, log_f.data_ptr(),
-             (_i64 * 2)(log_f.stride(0), log_f.stride(1)), self.dt, T, N, W, self.P, self.H, self.Hk, self.d,
+             None if log_f.is_contiguous() else (_i64 * 2)(log_f.stride(0), log_f.stride(1)), self.dt, T, N, W, self.P, self.H, self.Hk, self.d,
              cu.data_ptr(), past.data_ptr(), table.data_ptr(), self.buffer.data_ptr(), self.buffer.numel(),
              _ptr(flags))
 
@@ -398,26 +408,26 @@ class PagedCache:
         T = q.shape[0]
         if eps > 0.0:
             for name, t, heads in (("gamma_q", gamma_q, self.H), ("gamma_k", gamma_k, self.Hk)):
-                if t is None or t.shape != (heads,) or t.dtype != torch.float32 or t.device != dev \
+                if t is None or t.shape != (heads,) or t.dtype != torch.float32 or t.get_device() != dev \
                         or not t.is_contiguous():
                     raise ValueError(f"{name} must be float32 [{heads}]")
         else:
             gamma_q = gamma_k = None
         if out is None:
-            o = torch.empty((T, self.H, self.d), dtype=self.dtype, device=dev)
-            lse = torch.empty((T, self.H), dtype=torch.float32, device=dev)
+            o = q.new_empty((T, self.H, self.d))
+            lse = q.new_empty((T, self.H), dtype=torch.float32)
         else:
             o, lse = out
             if o.shape != (T, self.H, self.d) or o.dtype != self.dtype or lse.shape != (T, self.H) \
                     or lse.dtype != torch.float32 or not (o.is_contiguous() and lse.is_contiguous()) \
-                    or o.device != dev or lse.device != dev:
+                    or o.get_device() != dev or lse.get_device() != dev:
                 raise ValueError("out must be contiguous (O [T, H, d], lse [T, H])")
         if max_len is None:
             max_len = PAGE * W
         need = _sz(0)
         acp._check(lib().acp_paged_workspace_size(T, N, self.H, self.Hk, self.d, self.dt, max_new, max_len,
                                                   ctypes.byref(need)))
-        ws = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
+        ws = self.buffer.new_empty(need.value) if need.value else None
         _run(lib().fox_attn_paged, dev, q.data_ptr(), qs, self.dt, T, N, W, self.P, self.H, self.Hk, self.d,
              cu.data_ptr(), past.data_ptr(), table.data_ptr(), self.buffer.data_ptr(), self.buffer.numel(),
              _ptr(gamma_q), _ptr(gamma_k), eps, L_max, max_new, max_len, o.data_ptr(), lse.data_ptr(),
