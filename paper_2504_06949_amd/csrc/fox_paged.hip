@@ -839,23 +839,59 @@ void paged_long_kernel(PagedArgs, Work work, float kscale) {
 // ---- short -----------------------------------------------------------------------------
 template <typename T, int D>
 struct alignas(1024) ShortSmem {
-    // value tiles of each wave (bf16; float values go straight to registers)
-    unsigned char v[4][2][is_bf16<T>() ? 64 * D * 2 : 1024];
+    // value tiles of each wave (float values go straight to registers); at an item's end the
+    // wave's sums, [dt][lane]
+    unsigned char v[4][2][is_bf16<T>() ? 64 * D * 2 : D * 32];
     unsigned bad[4][2];
     unsigned inf[16][2][D / 32];
     int marked;
     float m[4][16], l[4][16];
-    int first[16];
     ShareSmem share;
 };
 
+// The gates of a page for the heads of a group, in LDS: 16-byte piece i of head k at position
+// i ^ k of its 32, so that a read of the same piece of all heads spreads over the banks.
+struct GateDma {
+    // bytes a wave needs for G heads
+    __host__ __device__ static constexpr int bytes(int G) { return (G + 1) / 2 * 1024; }
+    // src: the page's gates of the group's first head.  Two heads per instruction (of an odd
+    // count the last one twice).  Waited for as TileDma's loads.
+    static __device__ __forceinline__ void issue(unsigned char* to, const double* src, int G, int lane) {
+        typedef __attribute__((address_space(3))) unsigned char lds_u8;
+        const unsigned long long p = reinterpret_cast<unsigned long long>(src);
+        const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)p);
+        const unsigned hi = __builtin_amdgcn_readfirstlane((unsigned)(p >> 32));
+        const unsigned long long base = ((unsigned long long)hi << 32) | lo;
+        for (int k = 0; k < G; k += 2) {
+            const int head = k + (lane >> 5);
+            const unsigned off = min(head, G - 1) * 512 + (((lane & 31) ^ head) << 4);
+            const unsigned lds = __builtin_amdgcn_readfirstlane(
+                (unsigned)(unsigned long long)(const lds_u8*)(to + 512 * k));
+            asm volatile(
+                "s_mov_b32 m0, %0\n\t"
+                "s_nop 0\n\t"
+                "global_load_lds_dwordx4 %1, %2"
+                :
+                : "s"(lds), "v"(off), "s"(base)
+                : "memory", "m0");
+        }
+    }
+    static __device__ __forceinline__ double2 at(const unsigned char* from, int head, int piece) {
+        return *reinterpret_cast<const double2*>(from + head * 512 + ((piece ^ head) << 4));
+    }
+};
+
 // Rows r = token * G + head of the group, r < 16, are the queries of every wave.
+// gates_lds: the page's gates go through LDS (GateDma::bytes(G) more of it per wave), else each
+// lane loads those of its head and keys.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void paged_short_kernel(PagedArgs, Work work, float kscale) {
+__global__ __launch_bounds__(256, is_bf16<T>() && D == 64 ? 2 : 1) void paged_short_kernel(PagedArgs, Work work, float kscale,
+                                                                           bool gates_lds) {
     typedef RowBlock<T, D, 1> Block;
     constexpr int KH = is_bf16<T>() ? 2 : 1;            // halves of 32 keys per step
     constexpr int ND = D / 16;
     __shared__ ShortSmem<T, D> sm;
+    extern __shared__ __align__(16) unsigned char gates_s[];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wg = blockIdx.x;
     Share sh = find_share(work, wg, sm.share);
@@ -889,35 +925,23 @@ __global__ __launch_bounds__(256) void paged_short_kernel(PagedArgs, Work work, 
     // (all that the loops need of the arguments)
     const T* kp = (const T*)a.kp + (int64_t)hk * 64 * D;
     const T* vp = (const T*)a.vp + (int64_t)hk * 64 * D;
-    const double* gates = a.cp + (int64_t)h * 64;         // of the lane's head
+    const double* gates = a.cp + (int64_t)hk * G * 64;    // of the group's first head
     const int64_t page_stride = (int64_t)a.Hk * 64 * D, gate_stride = (int64_t)a.H * 64;
-    // What a step needs, requested one step ahead (bf16) or at its start (float)
+    const int head = r % G;
+    unsigned char* gate_tile = gates_s + (gates_lds ? wave * GateDma::bytes(G) : 0);
+    // What a step needs, requested one step ahead
     typename Block::Frag kf[KH][2][Block::NK];
-    double cj[KH][8], cend = 0.0;
     float vf[is_bf16<T>() ? 1 : ND][8];
     int page = -1;
     TileDma<D, 1> dma;
     if constexpr (is_bf16<T>()) dma.init(0, lane);
     PageWindow win;
 
-    auto load = [&](int n, int hf, int buf) __attribute__((always_inline)) {
+    auto load_rest = [&](int n, int hf, int buf) __attribute__((always_inline)) {
         const int p = win.get(a, s, n, lane);
         page = p;
         const int64_t at = max(p, 0) * page_stride;
-        const double* cp = gates + max(p, 0) * gate_stride;
-#pragma unroll
-        for (int ks = 0; ks < KH; ++ks) {
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-                for (int i = 0; i < Block::NK; ++i)
-                    kf[ks][kk][i] = *reinterpret_cast<const typename Block::Frag*>(
-                        kp + at + (int64_t)(32 * (ks + hf) + key_row<T>(kk, r16)) * D +
-                        4 * Block::kFrag * i + Block::kFrag * g);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) cj[ks][j] = cp[32 * (ks + hf) + key_of<T>(g, j)];
-        }
-        cend = cp[63];
+        if (gates_lds) GateDma::issue(gate_tile, gates + max(p, 0) * gate_stride, G, lane);
         if constexpr (is_bf16<T>()) {
             dma.issue(sm.v[wave][buf], vp + at, 0);
         } else {
@@ -928,40 +952,70 @@ __global__ __launch_bounds__(256) void paged_short_kernel(PagedArgs, Work work, 
                     vf[dt][j] = vp[at + (int64_t)(32 * hf + key_of<T>(g, j)) * D + 16 * dt + r16];
         }
     };
+    auto load_keys = [&](int hf) __attribute__((always_inline)) {
+        const int64_t at = max(page, 0) * page_stride;
+#pragma unroll
+        for (int ks = 0; ks < KH; ++ks)
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                for (int i = 0; i < Block::NK; ++i)
+                    kf[ks][kk][i] = *reinterpret_cast<const typename Block::Frag*>(
+                        kp + at + (int64_t)(32 * (ks + hf) + key_row<T>(kk, r16)) * D +
+                        4 * Block::kFrag * i + Block::kFrag * g);
+    };
 
     // wave w takes steps w, w + 4, .. of the part's pages (or half pages)
     const int steps = nb <= ne ? (ne - nb + 1) * (is_bf16<T>() ? 1 : 2) : 0;
     auto page_at = [&](int u) { return nb + (is_bf16<T>() ? u : u >> 1); };
     if (wave < steps) {
         win.fill(a, s, nb, lane);
-        load(page_at(wave), is_bf16<T>() ? 0 : wave & 1, 0);
+        load_rest(page_at(wave), is_bf16<T>() ? 0 : wave & 1, 0);
+        load_keys(is_bf16<T>() ? 0 : wave & 1);
     }
     int buf = 0;
     for (int u = wave; u < steps; u += 4, buf ^= 1) {
         const int n = page_at(u), hf = is_bf16<T>() ? 0 : u & 1;
-        if constexpr (is_bf16<T>()) wait_vmcnt0();
-        // this step's operands; the next step's are requested before they are used
-        typename Block::Frag kc[KH][2][Block::NK];
-        double cc[KH][8];
-        float vc[is_bf16<T>() ? 1 : ND][8];
-        const double end = cend;
         const int pg = page;
+        // The step's operands, each followed by the request for the next step's: c_i - c_j and
+        // the values in registers first, then the keys (none is held twice)
+        float decay[KH][8];
+        double end;
+        if (gates_lds) {
+            wait_vmcnt0();
 #pragma unroll
-        for (int ks = 0; ks < KH; ++ks) {
+            for (int ks = 0; ks < KH; ++ks)
 #pragma unroll
-            for (int kk = 0; kk < 2; ++kk)
+                for (int j = 0; j < 8; j += 2) {
+                    const double2 c = GateDma::at(gate_tile, head, (32 * (ks + hf) + key_of<T>(g, j)) >> 1);
+                    decay[ks][j] = (float)(ci - c.x);
+                    decay[ks][j + 1] = (float)(ci - c.y);
+                }
+            end = GateDma::at(gate_tile, head, 31).y;
+            asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+        } else {
+            const double* cp = gates + max(pg, 0) * gate_stride + head * 64;
 #pragma unroll
-                for (int i = 0; i < Block::NK; ++i) kc[ks][kk][i] = kf[ks][kk][i];
+            for (int ks = 0; ks < KH; ++ks)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) cc[ks][j] = cj[ks][j];
+                for (int j = 0; j < 8; ++j) decay[ks][j] = (float)(ci - cp[32 * (ks + hf) + key_of<T>(g, j)]);
+            end = cp[63];
+            wait_vmcnt0();
         }
+        float vc[is_bf16<T>() ? 1 : ND][8];
         if constexpr (!is_bf16<T>()) {
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) vc[dt][j] = vf[dt][j];
         }
-        if (u + 4 < steps) load(page_at(u + 4), is_bf16<T>() ? 0 : u & 1, buf ^ 1);
+        const int next_half = is_bf16<T>() ? 0 : u & 1;
+        if (u + 4 < steps) load_rest(page_at(u + 4), next_half, buf ^ 1);
+        f32x4 x[KH][2][1];
+#pragma unroll
+        for (int ks = 0; ks < KH; ++ks)
+            blk.scores(x[ks], [&](int kk, int i) __attribute__((always_inline)) { return kf[ks][kk][i]; });
+        if (u + 4 < steps) load_keys(next_half);
         if (pg < 0) {
             if (r16 < nrows) report(a, s, h, lane & 48);
             continue;
@@ -997,15 +1051,13 @@ __global__ __launch_bounds__(256) void paged_short_kernel(PagedArgs, Work work, 
         }
 #pragma unroll
         for (int ks = 0; ks < KH; ++ks) {
-            f32x4 x[2][1];
-            blk.scores(x, [&](int kk, int i) __attribute__((always_inline)) { return kc[ks][kk][i]; });
             float p[1][8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int key = 32 * (ks + hf) + key_of<T>(g, j);
                 const bool on = keep && 64 * n + key <= pi;
-                const float y = __builtin_fmaf(x[j >> 2][0][j & 3], kscale,
-                                               __builtin_fmaf((float)(ci - cc[ks][j]), kLog2e, -blk.ref[0]));
+                const float y = __builtin_fmaf(x[ks][j >> 2][0][j & 3], kscale,
+                                               __builtin_fmaf(decay[ks][j], kLog2e, -blk.ref[0]));
                 p[0][j] = on ? y : -INFINITY;
             }
             blk.weights(0, p[0]);
@@ -1035,18 +1087,18 @@ __global__ __launch_bounds__(256) void paged_short_kernel(PagedArgs, Work work, 
 #pragma unroll
     for (int w = 0; w < 4; ++w) L += sm.l[w][r16] * fast_exp2(sm.m[w][r16] - ref);
     const float scale = fast_exp2(blk.max_logit(0) - ref);
-    // [wave][dt][lane]; the first three waves' tiles are no longer read
-    __shared__ f32x4 o_s[3][ND][64];
+    // (a wave's tiles are no longer read)
+    auto o_s = [&](int w) __attribute__((always_inline)) { return reinterpret_cast<f32x4(*)[64]>(&sm.v[w][0][0]); };
     if (wave > 0)
 #pragma unroll
-        for (int dt = 0; dt < ND; ++dt) o_s[wave - 1][dt][lane] = blk.acc[0][dt] * scale;
+        for (int dt = 0; dt < ND; ++dt) o_s(wave)[dt][lane] = blk.acc[0][dt] * scale;
     __syncthreads();
     if (wave == 0) {
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) {
             f32x4 o = blk.acc[0][dt] * scale;
 #pragma unroll
-            for (int w = 0; w < 3; ++w) o += o_s[w][dt][lane];
+            for (int w = 1; w < 4; ++w) o += o_s(w)[dt][lane];
             blk.acc[0][dt] = o;
         }
         if (sm.marked) add_marks<D>(blk.acc[0], sm.inf[r16], g);
@@ -1242,8 +1294,13 @@ void attend(const PagedArgs& a, const Division& v, hipStream_t s) {
                        s, a, lw, sw, v.short_max, v.long_above, waves);
     if (v.long_on)
         hipLaunchKernelGGL((paged_long_kernel<T, D, NQ>), dim3(lw.wgs), dim3(256), 0, s, a, lw, kscale);
-    if (v.short_on)
-        hipLaunchKernelGGL((paged_short_kernel<T, D>), dim3(sw.wgs), dim3(256), 0, s, a, sw, kscale);
+    if (v.short_on) {
+        // (all of a CU's 160 KB hold the gates of 16 heads beside the values of d = 128, but no more)
+        const size_t gates = 4 * GateDma::bytes(G);
+        const bool fits = sizeof(ShortSmem<T, D>) + gates <= 160 * 1024;
+        hipLaunchKernelGGL((paged_short_kernel<T, D>), dim3(sw.wgs), dim3(256), fits ? gates : 0, s, a, sw, kscale,
+                           fits);
+    }
     if (lw.shared)
         hipLaunchKernelGGL((paged_join_kernel<T, D, 64 * NQ, true>), dim3(lw.wgs - 1, 4 * NQ), dim3(256), 0, s, a,
                            lw);
