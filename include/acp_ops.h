@@ -8,7 +8,8 @@
  *     {batch, head, position} (paged tensors: {token, head}); the features of a row
  *     are contiguous.  A null stride pointer means contiguous in the order stated.
  *     Strided tensors need only their element's alignment.  A stride is not negative.
- *   - Outputs must not overlap inputs unless said otherwise.
+ *   - Outputs must not overlap inputs unless said otherwise, nor each other; no two rows
+ *     of an output may share memory.
  */
 #ifndef ACP_OPS_H
 #define ACP_OPS_H
@@ -32,7 +33,8 @@ extern "C" {
  *        null); eps >= 0.
  *   out: y [B, H, L, n] dt, contiguous; mean (with center), rstd [B, H, L] float, or
  *        both null when no backward follows.
- * Supported: 1 <= n <= 16384; B*H*L < 2^31; B, H, L >= 0 (no row: nothing is done). */
+ * Supported: 1 <= n <= 16384; H <= 65535; B*H*L <= 2^30; B, H, L >= 0 (no row: nothing is
+ * done). */
 acp_status acp_norm_fwd(const void* x, const int64_t* x_strides, const void* weight,
                         const void* bias, acp_dtype dt, acp_dtype wdt, int B, int H, int L, int n,
                         int per_head, int center, double eps, void* y, float* mean, float* rstd,
@@ -86,7 +88,8 @@ acp_status acp_rotary_table(int rot, double base, int scaling, double factor, do
  *        pos_strides {batch, position} (0 allowed), or null: position l is start + l.
  *        inverse != 0 turns by the negative angle: the gradient (amplitude included).
  *   out: q_out, k_out dt, strided; each may be its input (same pointer and strides).
- * Supported: even d, rot <= d <= 1024; |position| < 2^31. */
+ * Supported: even d, rot <= d <= 1024; |position| < 2^31; H + Hk <= 65535;
+ * B*L*(d/8 + 2) < 2^32. */
 acp_status acp_rotary(const void* q, const int64_t* q_strides, const void* k,
                       const int64_t* k_strides, acp_dtype dt, int B, int H, int Hk, int L, int d,
                       int rot, int layout, int inverse, double amplitude, const double* turns,
@@ -115,7 +118,8 @@ acp_status acp_rotary(const void* q, const int64_t* q_strides, const void* k,
  * all device memory.  A page number outside [0, P), or a position beyond 64 W, is not
  * followed: what would be stored is dropped, what would be read is left out, and bit 6
  * of the sequence's flags is set (flags: [N, H] int32, overwritten; null: not reported;
- * bits as in acp.h).  A row outside [0, T) is not touched. */
+ * bits as in acp.h).  A row outside [0, T) is not touched.
+ * Supported: N <= 65535, T*H <= 2^26, N*H <= 2^22. */
 typedef struct {
     size_t k;          /* [P,Hk,64,d] dt    */
     size_t v;          /* [P,Hk,64,d] dt    */
@@ -145,10 +149,15 @@ acp_status acp_paged_append(const void* k, const int64_t* k_strides, const void*
  * n < i / 64 is left out where c_i - c_{64 n + 63} < delta, delta = -(2 U + log L_max - log eps),
  * U = gamma_q[h] gamma_k[h / (H / Hk)] sqrt(d) (App. E, App. F: the row-wise block test of
  * fox_attn_decode); eps = 0 leaves nothing out and gamma_q, gamma_k may be null.
+ * The entries of pages that no row keeps any more may be set to -1 (and the pages used anew):
+ * with eps > 0 the search for a row's first kept page takes an entry out of range for a page
+ * that the test leaves out, and with it the pages before it, and reports neither.  An entry
+ * out of range after that page is reported.
  *   in : q [T, H, d] dt (strided, 16-byte aligned rows); gamma_q [H], gamma_k [Hk] float.
  *        max_new bounds cu[s + 1] - cu[s] and max_len past[s] plus that; they choose
  *        the division of the work and size the workspace.  The rows of a sequence with
- *        more than max_new may be left as they are (flag bit 7); max_len is a hint.
+ *        more than max_new may be left as they are (flag bit 7 says they were); max_len is a
+ *        hint that any value may have.
  *   out: O [T, H, d] dt, lse [T, H] float, contiguous; a row all of whose keys were
  *        left out by bad pages gets O = 0, lse = -inf.
  *   ws : acp_paged_workspace_size() bytes.

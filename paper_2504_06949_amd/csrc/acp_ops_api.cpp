@@ -52,7 +52,7 @@ acp_status check_rows(int B, int H, int L, int n) {
         return set_error(ACP_EINVAL, "bad sizes (B=%d H=%d L=%d n=%d)", B, H, L, n);
     if (n > 16384) return set_error(ACP_EUNSUPPORTED, "n=%d exceeds 16384", n);
     const double rows = (double)B * H * L;
-    if (rows > 2147483647.0) return set_error(ACP_EUNSUPPORTED, "B*H*L=%.0f exceeds 2^31 - 1", rows);
+    if (rows > 1073741824.0) return set_error(ACP_EUNSUPPORTED, "B*H*L=%.0f exceeds 2^30", rows);
     if (H > 65535) return set_error(ACP_EUNSUPPORTED, "H=%d exceeds 65535", H);
     return ACP_OK;
 }
@@ -80,10 +80,19 @@ acp_paged_layout paged_layout(int P, int H, int Hk, int d, acp_dtype dt) {
     return y;
 }
 
-acp_status check_call(int T, int N, int W, const void* cu, const void* past, const void* table) {
-    if (T < 0 || N < 0 || W < 0) return set_error(ACP_EINVAL, "bad sizes (T=%d N=%d W=%d)", T, N, W);
-    if (T > 1 << 26 || N > 65535)
-        return set_error(ACP_EUNSUPPORTED, "T=%d exceeds 2^26 or N=%d exceeds 65535", T, N);
+// (bounds under which no launch of the paged operators has 2^32 threads)
+acp_status check_sequences(int T, int N, int H) {
+    if (T < 0 || N < 0) return set_error(ACP_EINVAL, "bad sizes (T=%d N=%d)", T, N);
+    if (N > 65535) return set_error(ACP_EUNSUPPORTED, "N=%d exceeds 65535", N);
+    if ((int64_t)T * H > 1 << 26 || (int64_t)N * H > 1 << 22)
+        return set_error(ACP_EUNSUPPORTED, "T*H=%lld exceeds 2^26 or N*H=%lld exceeds 2^22", (long long)T * H,
+                         (long long)N * H);
+    return ACP_OK;
+}
+
+acp_status check_call(int T, int N, int W, int H, const void* cu, const void* past, const void* table) {
+    if (W < 0) return set_error(ACP_EINVAL, "bad size W=%d", W);
+    ACP_TRY(check_sequences(T, N, H));
     ACP_TRY(check_ptr(cu, "cu", 4));
     if (N > 0) ACP_TRY(check_ptr(past, "past", 4));
     if (N > 0 && W > 0) ACP_TRY(check_ptr(table, "table", 4));
@@ -122,11 +131,9 @@ acp::PagedArgs paged_args(acp_dtype dt, int T, int N, int W, int P, int H, int H
     return a;
 }
 
-acp_status check_division(int T, int N, int H, int max_new, int64_t max_len) {
+acp_status check_division(int max_new, int64_t max_len) {
     if (max_new < 0 || max_len < 0 || max_len > ((int64_t)1 << 31))
         return set_error(ACP_EINVAL, "max_new=%d or max_len=%lld outside their range", max_new, (long long)max_len);
-    if ((int64_t)T * H > (int64_t)1 << 28 || (int64_t)N * H > (int64_t)1 << 28)
-        return set_error(ACP_EUNSUPPORTED, "T*H=%lld or N*H=%lld exceeds 2^28", (long long)T * H, (long long)N * H);
     return ACP_OK;
 }
 
@@ -165,7 +172,7 @@ acp_status acp_norm_fwd(const void* x, const int64_t* x_strides, const void* wei
 acp_status acp_norm_workspace_size(int B, int H, int L, int n, int per_head, size_t* bytes) {
     ACP_TRY(check_rows(B, H, L, n));
     if (bytes == nullptr) return set_error(ACP_EINVAL, "bytes is NULL");
-    *bytes = acp::norm_workspace(B, H, L, n, per_head != 0);
+    *bytes = H == 0 ? 0 : acp::norm_workspace(B, H, L, n, per_head != 0);
     return ok();
 }
 
@@ -252,9 +259,10 @@ acp_status acp_rotary(const void* q, const int64_t* q_strides, const void* k, co
     if (rot < 2 || rot % 2 != 0 || rot > d) return set_error(ACP_EINVAL, "rot=%d is not even in [2, d=%d]", rot, d);
     if (layout != ACP_ROTARY_HALF && layout != ACP_ROTARY_INTERLEAVED)
         return set_error(ACP_EINVAL, "unknown layout %d", layout);
-    if (!std::isfinite(amplitude)) return set_error(ACP_EINVAL, "amplitude is not finite");
-    if ((double)B * L > 2147483647.0 || H + (int64_t)Hk > 65535)
-        return set_error(ACP_EUNSUPPORTED, "B*L exceeds 2^31 - 1 or H + Hk exceeds 65535");
+    if (!std::isfinite((float)amplitude)) return set_error(ACP_EINVAL, "amplitude is not finite");
+    // (threads of a launch: fewer than d / 8 + 2 chunks per position)
+    if ((double)B * L * (d / 8 + 2) >= 4294967296.0 || H + (int64_t)Hk > 65535)
+        return set_error(ACP_EUNSUPPORTED, "B*L*(d/8 + 2) reaches 2^32 or H + Hk exceeds 65535");
     if ((int64_t)B * L == 0 || H + Hk == 0) return ok();
     if (q == nullptr && k == nullptr) return set_error(ACP_EINVAL, "q and k are NULL");
     acp::RotaryArgs a{};
@@ -276,6 +284,7 @@ acp_status acp_rotary(const void* q, const int64_t* q_strides, const void* k, co
         a.x[w] = in[w]; a.y[w] = out[w]; a.heads[w] = n;
         heads += n;
     }
+    if (q && k && q_out == k_out && H > 0 && Hk > 0) return set_error(ACP_EINVAL, "k_out is q_out");
     ACP_TRY(check_ptr(turns, "turns", 8));
     if (positions) {
         if (pos_bytes != 4 && pos_bytes != 8) return set_error(ACP_EINVAL, "pos_bytes=%d is not 4 or 8", pos_bytes);
@@ -283,7 +292,7 @@ acp_status acp_rotary(const void* q, const int64_t* q_strides, const void* k, co
         if (pos_strides == nullptr) return set_error(ACP_EINVAL, "pos_strides is NULL");
         if (pos_strides[0] < 0 || pos_strides[1] < 0) return set_error(ACP_EINVAL, "positions has a negative stride");
         a.pos_b = pos_strides[0]; a.pos_l = pos_strides[1];
-    } else if (start <= -(INT64_C(1) << 31) || start + L > (INT64_C(1) << 31)) {
+    } else if (start <= -(INT64_C(1) << 31) || start > (INT64_C(1) << 31) - L) {
         return set_error(ACP_EINVAL, "start=%lld outside (-2^31, 2^31 - L]", (long long)start);
     }
     if (heads == 0) return ok();
@@ -317,7 +326,7 @@ acp_status acp_paged_append(const void* k, const int64_t* k_strides, const void*
                             const int32_t* table, void* cache, size_t cache_bytes, int32_t* flags,
                             void* stream) {
     ACP_TRY(check_paged(P, H, Hk, d, dt));
-    ACP_TRY(check_call(T, N, W, cu, past, table));
+    ACP_TRY(check_call(T, N, W, H, cu, past, table));
     ACP_TRY(check_cache(cache, cache_bytes, paged_layout(P, H, Hk, d, dt)));
     if (flags) ACP_TRY(check_ptr(flags, "flags", 4));
     acp::PagedArgs a = paged_args(dt, T, N, W, P, H, Hk, d, cu, past, table, cache, flags);
@@ -343,8 +352,8 @@ acp_status acp_paged_append(const void* k, const int64_t* k_strides, const void*
 acp_status acp_paged_workspace_size(int T, int N, int H, int Hk, int d, acp_dtype dt, int max_new,
                                     int64_t max_len, size_t* bytes) {
     ACP_TRY(check_paged(1, H, Hk, d, dt));
-    if (T < 0 || N < 0) return set_error(ACP_EINVAL, "bad sizes (T=%d N=%d)", T, N);
-    ACP_TRY(check_division(T, N, H, max_new, max_len));
+    ACP_TRY(check_sequences(T, N, H));
+    ACP_TRY(check_division(max_new, max_len));
     if (bytes == nullptr) return set_error(ACP_EINVAL, "bytes is NULL");
     acp::PagedArgs a{};
     a.bf16 = dt == ACP_BF16;
@@ -360,9 +369,9 @@ acp_status fox_attn_paged(const void* q, const int64_t* q_strides, acp_dtype dt,
                           double eps, int64_t L_max, int max_new, int64_t max_len, void* O, float* lse,
                           int32_t* flags, void* ws, size_t ws_bytes, void* stream) {
     ACP_TRY(check_paged(P, H, Hk, d, dt));
-    ACP_TRY(check_call(T, N, W, cu, past, table));
+    ACP_TRY(check_call(T, N, W, H, cu, past, table));
     ACP_TRY(check_cache(cache, cache_bytes, paged_layout(P, H, Hk, d, dt)));
-    ACP_TRY(check_division(T, N, H, max_new, max_len));
+    ACP_TRY(check_division(max_new, max_len));
     if (!std::isfinite(eps) || eps < 0.0 || eps >= 1.0) return set_error(ACP_EINVAL, "eps=%g outside [0, 1)", eps);
     if (eps > 0.0) {
         if (L_max < 1 || L_max > (INT64_C(1) << 31))

@@ -24,6 +24,7 @@ import os
 import re
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import acp
 from .acp import ACP_BF16, ACP_F32, AcpError
@@ -222,6 +223,7 @@ class _Norm(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, weight, mean, rstd = ctx.saved_tensors
         dx, dw, db = norm_backward(dy.to(x.dtype), x, weight, mean, rstd, ctx.has_bias)
@@ -321,6 +323,7 @@ class _Rotate(torch.autograd.Function):
         return rope.forward(_features(q), _features(k), positions, start)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dq, dk):
         positions, = ctx.saved_tensors
         dq, dk = ctx.rope.backward(_features(dq), _features(dk) if ctx.two else None, positions, ctx.start)

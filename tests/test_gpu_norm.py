@@ -7,7 +7,7 @@ half a step of their type.  A weight's gradient adds chains of up to 250 terms."
 import pytest
 import torch
 
-from paper_2504_06949_amd import ops
+from paper_2504_06949_amd import acp, ops
 from tests._helpers import ensure_built
 
 pytestmark = pytest.mark.gpu
@@ -202,3 +202,58 @@ def test_dx_in_place_of_dy_and_row_offsets_past_31_bits():
     y, _, _ = ops.norm_forward(rows, w)
     want, _, _ = ops.norm_forward(src, w)
     assert torch.equal(y.view(3, 128), want)
+
+
+@pytest.mark.parametrize("n", [3, 64, 257, 1025, 6000])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_dx_over_dy(n, dtype):
+    """dx written over dy (pieces of an odd width overlap): the same as beside it."""
+    x, w = _x((37, n), dtype), _w(n)
+    dy = _x((37, n), dtype, seed=7)
+    _, mean, rstd = ops.norm_forward(x, w, center=True)
+    want = ops.norm_backward(dy, x, w, mean, rstd)
+    dw, ws = torch.empty(n, device="cuda"), torch.empty(1 << 22, device="cuda")
+    place = dy.clone()
+    dt = acp.ACP_BF16 if dtype == torch.bfloat16 else acp.ACP_F32
+    stream = torch.cuda.current_stream().cuda_stream
+    assert ops.lib().acp_norm_bwd(place.data_ptr(), None, x.data_ptr(), None, w.data_ptr(), dt, acp.ACP_F32, 1, 1,
+                                  37, n, 0, mean.data_ptr(), rstd.data_ptr(), place.data_ptr(), None, dw.data_ptr(),
+                                  None, ws.data_ptr(), 4 * ws.numel(), stream) == acp.ACP_OK
+    assert torch.equal(place, want[0]) and torch.equal(dw, want[1])
+
+
+def test_no_heads():
+    x, w = torch.empty((2, 0, 3, 64), device="cuda"), torch.empty((0, 64), device="cuda")
+    y, mean, rstd = ops.norm_forward(x, w, w, center=True)
+    dx, dw, db = ops.norm_backward(x, x, w, mean, rstd, bias=True)
+    assert y.shape == dx.shape == x.shape and dw.shape == db.shape == w.shape
+
+
+def test_captured_step():
+    """Forward and backward in a graph, replayed with new contents between eager calls."""
+    x, dy, w = _x((2, 4, 300, 64), torch.bfloat16), _x((2, 4, 300, 64), torch.bfloat16, seed=8), _w((4, 64))
+
+    def step():
+        y, mean, rstd = ops.norm_forward(x, w, w, center=True)
+        return (y,) + ops.norm_backward(dy, x, w, mean, rstd, bias=True)
+
+    step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for _ in range(3):
+        x.copy_(x.roll(1, 2))
+        dy.copy_(dy.roll(3, 2))
+        want = step()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, want):
+            assert torch.equal(a, b)
+
+
+def test_second_derivatives_are_refused():
+    x, w = _x((5, 64), torch.float32).requires_grad_(True), _w(64)
+    g, = torch.autograd.grad(ops.rms_norm(x, w).sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.sum().backward()

@@ -408,3 +408,72 @@ def test_another_stream_and_a_captured_step():
             g.replay()
             torch.cuda.synchronize()
             assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1]), r
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_sixteen_query_heads_of_128_features(dtype):
+    """The most query heads per key head beside the widest rows, as single tokens and a chunk."""
+    for new, past in (([1, 1], [700, 63]), ([20, 1], [300, 64])):
+        serve(World(new, past, 32, 2, 128, dtype, seed=16, mu=(0.0, 7.0)))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("new,past", [([1], [60000]), ([100], [20000]), ([3, 1], [30000, 1])])
+def test_long_sequences_in_many_shares(new, past, dtype):
+    """Few rows over many pages: their sums are merged from dozens of workgroups."""
+    w = World(new, past, 2, 1, 64, dtype, seed=17, mu=(9.0, 11.0))
+    w.fill_past()
+    w.append()
+    for eps in (0.0, EPS):
+        w.check(*w.attend(eps, L_max=1 << 16), eps=eps, L_max=1 << 16)
+
+
+@pytest.mark.parametrize("max_len", [1 << 12, 64])
+def test_many_ragged_sequences(max_len):
+    """More (sequence, head) items than are shared out, and as many that are, some without a
+    row; then all of them with a chunk."""
+    N = 1100
+    new = [(0, 1, 1, 2, 1, 5, 1)[i % 7] for i in range(N)]
+    past = [(i * 37) % 180 for i in range(N)]
+    w = World(new, past, 4, 4, 64, BF, seed=18, mu=(1.0, 6.0))
+    w.fill_past()
+    w.append()
+    some = [0, 1, 2, 3, 5, 6, 550, 1095, 1096, 1099]
+    w.check(*w.attend(max_len=max_len), seqs=some)
+    new = [(0, 1, 33, 70)[i % 4] for i in range(300)]
+    w = World(new, [(i * 41) % 900 for i in range(300)], 8, 2, 64, BF, seed=19, mu=(1.0, 6.0))
+    w.fill_past()
+    w.append()
+    w.check(*w.attend(max_len=max_len), seqs=[0, 1, 2, 3, 150, 151, 297, 298, 299])
+
+
+def test_two_calls_at_once():
+    """Calls on two streams at a time read the same cache and keep to their own scratch."""
+    w = World([1, 40, 1, 9], [3000, 800, 64, 100], 4, 2, 64, BF, seed=20, mu=(5.0, 8.0))
+    o, lse = serve(w)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = []
+    for st in streams:
+        st.wait_stream(torch.cuda.current_stream())
+    for _ in range(5):
+        for st in streams:
+            with torch.cuda.stream(st):
+                outs.append(w.attend())
+    for st in streams:
+        torch.cuda.current_stream().wait_stream(st)
+    for a, b in outs:
+        assert torch.equal(a, o) and torch.equal(b, lse)
+
+
+def test_operator_timing_counts_calls():
+    w = World([1, 30], [100, 20], 2, 2, 64, BF, seed=21)
+    acp.acp_timing_reset()
+    acp.acp_timing_enable(True)
+    try:
+        serve(w)
+    finally:
+        acp.acp_timing_enable(False)
+    t = ops.acp_op_timing_read()
+    acp.acp_timing_reset()
+    assert t["append"][0] == 2 and t["attend"][0] == 1 and t["norm"] == (0, 0.0)
+    assert 0.0 < t["attend"][1] < 1000.0 and 0.0 < t["append"][1] < 1000.0

@@ -139,3 +139,39 @@ def test_autograd():
     one = _x((2, 3, 20, 64), torch.float32, 1).requires_grad_(True)
     rope(one)[0].sum().backward()
     close(one.grad, turn(torch.ones_like(one), rope, pos[None], True), 64)
+
+
+def test_captured_step():
+    """Turned in place and back in a graph, replayed with new contents between eager calls."""
+    rope = ops.Rotary(64)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q = torch.randn((1, 4, 70, 64), generator=g, device="cuda").bfloat16()
+    k = torch.randn((1, 2, 70, 64), generator=g, device="cuda").bfloat16()
+    pos = torch.arange(70, device="cuda")
+
+    def step():
+        a, b = rope.forward(q, k, pos)
+        return a, b, *rope.backward(a, b, pos)
+
+    step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for _ in range(3):
+        q.copy_(q.roll(1, 2))
+        k.copy_(k.roll(1, 2))
+        pos.add_(1000)
+        want = step()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, want):
+            assert torch.equal(a, b)
+
+
+def test_second_derivatives_are_refused():
+    rope = ops.Rotary(64)
+    q = torch.ones((1, 1, 3, 64), device="cuda", requires_grad=True)
+    g, = torch.autograd.grad((rope(q)[0] ** 2).sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.sum().backward()

@@ -197,6 +197,34 @@ def test_tensor_helpers_refuse_cpu_tensors():
         ops.PagedCache(4, 4, 64, dtype=torch.float16, device="cpu")
 
 
+@pytest.mark.parametrize("call,status", [
+    (lambda: _norm_fwd(B=1 << 15, L=(1 << 15) + 1, H=1), acp.ACP_EUNSUPPORTED),
+    (lambda: _norm_fwd(B=46340, L=46340, H=1, n=1), acp.ACP_EUNSUPPORTED),      # just under 2^31
+    (lambda: _rotary(pos=None, start=(1 << 63) - 1), acp.ACP_EINVAL),
+    (lambda: _rotary(pos=None, start=(1 << 31) - 2), acp.ACP_EINVAL),
+    (lambda: _rotary(ko=48), acp.ACP_EINVAL),                                    # both into one place
+    (lambda: _rotary(amp=1e300), acp.ACP_EINVAL),
+    (lambda: _rotary(B=1 << 15, L=1 << 14, d=64), acp.ACP_EUNSUPPORTED),
+    (lambda: _append(T=1 << 25, H=4), acp.ACP_EUNSUPPORTED),
+    (lambda: _append(N=65535, H=128, Hk=128), acp.ACP_EUNSUPPORTED),
+    (lambda: _attend(N=65535, H=128, Hk=128), acp.ACP_EUNSUPPORTED),
+    (lambda: _attend(T=1 << 25), acp.ACP_EUNSUPPORTED),
+    (lambda: _attend(max_len=(1 << 31) + 1), acp.ACP_EINVAL),
+])
+def test_bounds_of_sizes(call, status):
+    """Counts that an int or a launch could not hold are refused."""
+    assert call() == status and acp.acp_last_error() != ""
+
+
+def test_workspace_sizes_of_empty_calls():
+    n = ctypes.c_size_t(7)
+    for B, H, L, per in ((0, 3, 5, 1), (2, 0, 5, 1), (2, 0, 5, 0), (2, 3, 0, 1)):
+        assert ops.lib().acp_norm_workspace_size(B, H, L, 64, per, ctypes.byref(n)) == acp.ACP_OK
+        assert n.value == 0
+    for T, N in ((0, 0), (0, 3), (5, 0)):
+        assert ops.lib().acp_paged_workspace_size(T, N, 4, 2, 64, 1, 0, 0, ctypes.byref(n)) == acp.ACP_OK
+
+
 def test_operator_timing_without_launches():
     acp.acp_timing_reset()
     assert ops.acp_op_timing_read() == {n: (0, 0.0) for n in ops.OP_NAMES}
