@@ -477,3 +477,11 @@ def test_operator_timing_counts_calls():
     acp.acp_timing_reset()
     assert t["append"][0] == 2 and t["attend"][0] == 1 and t["norm"] == (0, 0.0)
     assert 0.0 < t["attend"][1] < 1000.0 and 0.0 < t["append"][1] < 1000.0
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d,scale", [(64, 2.1), (64, 2.5), (64, 2.6), (128, 2.1), (128, 2.2)])
+def test_scales_on_both_sides_of_a_known_reference(d, scale, dtype):
+    """U = scale^2 sqrt(d) above 32 (35 to 50) and above 52: the two ways in which the weights of
+    a chunk are kept in float32's range."""
+    serve(World([100, 1], [300, 200], 2, 1, d, dtype, seed=22, scale=scale, mu=(2.0, 7.0)))
