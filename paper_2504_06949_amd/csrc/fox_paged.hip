@@ -1167,18 +1167,22 @@ __global__ __launch_bounds__(256, is_bf16<T>() && D == 64 ? 2 : 1) void paged_sh
 // The partial sums of an item that lies in several shares, of R rows per slot.  A workgroup
 // per share, for the item whose first cut lies at the share's start, and per 16 rows: 16 lanes
 // take a row (four rows of a slot in one load of a wave), or, of fewer rows, every so many
-// lanes' parts of it.
-template <typename T, int D, int R, bool kLong>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a, Work w) {
+// lanes' parts of it.  The first long_wgs workgroups merge long items, the others short ones.
+template <typename T, int D, int kLongRows>
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a, Work lw, Work sw, int long_wgs) {
     constexpr int kPer = D / 64;                         // features 64 k + 4 l .. + 3 of lane l
     __shared__ float sm[16][D + 2];
-    const int wg = blockIdx.x + 1;
+    const bool is_long = (int)blockIdx.x < long_wgs;
+    const Work w = is_long ? lw : sw;
+    constexpr int kTiles = kLongRows / 16;
+    const int R = is_long ? kLongRows : kShortRows;
+    const int wg = 1 + (is_long ? (int)blockIdx.x / kTiles : (int)blockIdx.x - long_wgs);
     const Cut cut = w.cuts[wg];
     if (cut.item < 0) return;
     const int id = cut.item;
     const Item it = w.items[id];
-    const int G = a.H / a.Hk, r0 = 16 * blockIdx.y;
-    const int rows = min(16, (kLong ? it.n : it.n * G) - r0);
+    const int G = a.H / a.Hk, r0 = is_long ? 16 * ((int)blockIdx.x % kTiles) : 0;
+    const int rows = min(16, (is_long ? it.n : it.n * G) - r0);
     if (rows <= 0) return;
     // the share before has its first pages; its last one lies here or in a later share
     const int w0 = wg - 1, parts = 2 + (w.setup - cut.skip + it.pages - 1) / cut.chunk;
@@ -1241,8 +1245,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a, Work w) {
         }
     }
     if (!on) return;
-    const int h = kLong ? long_head(a, id, w.tiles) : id / w.tiles * G + r % G;
-    const int64_t row = (int64_t)(it.t0 + (kLong ? r : r / G)) * a.H + h;
+    const int h = is_long ? long_head(a, id, w.tiles) : id / w.tiles * G + r % G;
+    const int64_t row = (int64_t)(it.t0 + (is_long ? r : r / G)) * a.H + h;
     const float inv = L == 0.f ? 0.f : 1.0f / L;
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
@@ -1351,11 +1355,10 @@ void attend(const PagedArgs& a, const Division& v, hipStream_t s) {
         hipLaunchKernelGGL((paged_short_kernel<T, D>), dim3(sw.wgs), dim3(256), fits ? gates : 0, s, a, sw, kscale,
                            fits);
     }
-    if (lw.shared)
-        hipLaunchKernelGGL((paged_join_kernel<T, D, 64 * NQ, true>), dim3(lw.wgs - 1, 4 * NQ), dim3(256), 0, s, a,
-                           lw);
-    if (sw.shared)
-        hipLaunchKernelGGL((paged_join_kernel<T, D, kShortRows, false>), dim3(sw.wgs - 1), dim3(256), 0, s, a, sw);
+    const int long_wgs = lw.shared ? (lw.wgs - 1) * 4 * NQ : 0, short_wgs = sw.shared ? sw.wgs - 1 : 0;
+    if (long_wgs + short_wgs > 0)
+        hipLaunchKernelGGL((paged_join_kernel<T, D, 64 * NQ>), dim3(long_wgs + short_wgs), dim3(256), 0, s, a, lw,
+                           sw, long_wgs);
 }
 template <typename T, int D>
 void attend(const PagedArgs& a, const Division& v, hipStream_t s) {
