@@ -130,6 +130,11 @@ def _strides(t: torch.Tensor):
     return (_i64 * 3)(s[0], s[1], s[2])
 
 
+def _contiguous_like(t: torch.Tensor) -> torch.Tensor:
+    """An empty contiguous tensor like t (empty_like where it is one: 0.6 us less than new_empty)."""
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -173,7 +178,7 @@ def norm_forward(x, weight, bias=None, eps: float = 1e-6, center: bool = False, 
     if not weight.is_contiguous() or (bias is not None and not bias.is_contiguous()):
         raise ValueError("weight and bias must be contiguous")
     B, H, L, n = x4.shape
-    y = x.new_empty(x.shape) if out is None else out
+    y = _contiguous_like(x) if out is None else out
     if out is not None and (out.shape != x.shape or out.dtype != x.dtype or not out.is_contiguous()
                             or out.get_device() != dev):
         raise ValueError("out must be contiguous and like x")
@@ -288,7 +293,7 @@ class Rotary:
             raise ValueError("q must be [B, H, L, d] and k [B, Hk, L, d] of its type")
         B, H, L, d = q.shape
         if out is None:
-            out = (q.new_empty(q.shape), None if k is None else k.new_empty(k.shape))
+            out = (_contiguous_like(q), None if k is None else _contiguous_like(k))
         for t, o in zip((q, k), out):
             if t is None:
                 continue
@@ -354,15 +359,16 @@ class PagedCache:
         n = _sz(0)
         acp._check(lib().acp_paged_cache_size(pages, H, self.Hk, d, self.dt, ctypes.byref(n)))
         self.buffer = torch.empty(n.value, dtype=torch.uint8, device=device)
+        y = PagedLayout()
+        acp._check(lib().acp_paged_offsets(pages, H, self.Hk, d, self.dt, ctypes.byref(y)))
+        kv = (pages, self.Hk, PAGE, d)
+        self._views = {"k": self.buffer[y.k:y.v].view(dtype).view(kv),
+                       "v": self.buffer[y.v:y.c].view(dtype).view(kv),
+                       "c": self.buffer[y.c:y.total].view(torch.float64).view(pages, H, PAGE)}
 
     def views(self) -> dict:
         """Views of the pages: k, v [P, Hk, 64, d], c [P, H, 64] float64."""
-        y = PagedLayout()
-        acp._check(lib().acp_paged_offsets(self.P, self.H, self.Hk, self.d, self.dt, ctypes.byref(y)))
-        kv = (self.P, self.Hk, PAGE, self.d)
-        return {"k": self.buffer[y.k:y.v].view(self.dtype).view(kv),
-                "v": self.buffer[y.v:y.c].view(self.dtype).view(kv),
-                "c": self.buffer[y.c:y.total].view(torch.float64).view(self.P, self.H, PAGE)}
+        return dict(self._views)
 
     def _sequences(self, cu, past, table, flags):
         for name, t in (("cu", cu), ("past", past), ("table", table), ("flags", flags)):
@@ -395,9 +401,9 @@ class PagedCache:
         if v.shape[0] != T or log_f.shape != (T, self.H) or log_f.dtype != torch.float32:
             raise ValueError("v must be like k, and log_f float32 [T, H]")
         _run(lib().acp_paged_append, dev, k.data_ptr(), ks, v.data_ptr(), vs, log_f.data_ptr(),
-             None if log_f.is_contiguous() else (_i64 * 2)(log_f.stride(0), log_f.stride(1)), self.dt, T, N, W, self.P, self.H, self.Hk, self.d,
-             cu.data_ptr(), past.data_ptr(), table.data_ptr(), self.buffer.data_ptr(), self.buffer.numel(),
-             _ptr(flags))
+             None if log_f.is_contiguous() else (_i64 * 2)(log_f.stride(0), log_f.stride(1)), self.dt, T, N, W,
+             self.P, self.H, self.Hk, self.d, cu.data_ptr(), past.data_ptr(), table.data_ptr(),
+             self.buffer.data_ptr(), self.buffer.numel(), _ptr(flags))
 
     def attend(self, q, cu, past, table, max_new: int, max_len: int | None = None, gamma_q=None,
                gamma_k=None, eps: float = 0.0, L_max: int = 131072, out=None, flags=None):
@@ -417,7 +423,7 @@ class PagedCache:
         else:
             gamma_q = gamma_k = None
         if out is None:
-            o = q.new_empty((T, self.H, self.d))
+            o = _contiguous_like(q)
             lse = q.new_empty((T, self.H), dtype=torch.float32)
         else:
             o, lse = out
