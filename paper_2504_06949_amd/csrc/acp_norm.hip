@@ -370,13 +370,23 @@ __global__ __launch_bounds__(norm_threads<LPR>()) void norm_bwd_kernel(
 __global__ __launch_bounds__(1024) void norm_sum_kernel(
     const float* __restrict__ part_w, const float* __restrict__ part_b, int parts, int n,
     float* __restrict__ dw, float* __restrict__ db) {
+    constexpr int kAtOnce = 8;
     __shared__ float s[64][17];
     const float* part = blockIdx.z ? part_b : part_w;
     float* out = blockIdx.z ? db : dw;
     const int g = blockIdx.y, c = blockIdx.x * 16 + (threadIdx.x & 15), k0 = threadIdx.x >> 4;
     float t = 0.f;
     if (c < n)
-        for (int k = k0; k < parts; k += 64) t += part[((int64_t)g * parts + k) * n + c];
+        // (kAtOnce loads in flight)
+        for (int k = k0; k < parts; k += 64 * kAtOnce) {
+            float v[kAtOnce];
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i)
+                v[i] = part[((int64_t)g * parts + min(k + 64 * i, parts - 1)) * n + c];
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i)
+                if (k + 64 * i < parts) t += v[i];
+        }
     s[k0][threadIdx.x & 15] = t;
     __syncthreads();
 #pragma unroll
