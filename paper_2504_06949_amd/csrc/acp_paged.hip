@@ -3,7 +3,8 @@
 //
 // One launch holds two kinds of workgroups that touch different memory: the first ones sum
 // the gates of a sequence (a few heads each), the others copy the rows of a few tokens.  Bound
-// by memory: each row is read and written once.
+// by memory: each row is read and written once.  Ragged 32k tokens of 12 heads (d = 64,
+// bfloat16): 35 to 44 us for 206 MB.
 #include "acp_paged.h"
 #include "acp_scan.h"
 
@@ -16,8 +17,9 @@ constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
 constexpr int kFewTokens = 16;                       // summed one after the other
 // Heads per workgroup of the sums: one where sequences are long (issue on the one CU that
-// holds a workgroup bounds them: four heads took 60 us where one takes the 50 us of the
-// copies, ragged 32k tokens of 12 heads), four where there are more sequences than CUs
+// holds a workgroup bounds them: four heads took 60 us where one was hidden behind the 50 us
+// that the copies then took, ragged 32k tokens of 12 heads), four where there are more
+// sequences than CUs
 constexpr int kGateHeadsLong = 1, kGateHeadsShort = 4;
 static_assert(kWaves * kGateHeadsShort == 64, "a total per lane");
 

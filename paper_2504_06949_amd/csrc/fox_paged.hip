@@ -7,11 +7,17 @@
 // softmax per query, and O^T += V^T P^T.
 //   paged_long_kernel   64 or 128 rows of one head per workgroup, 16 or 32 per wave; the
 //                       waves share the pages in LDS.  Bound by the matrix cores and the
-//                       exponentials.
+//                       exponentials, which overlap in part: 8000 rows of 16 heads (4 key heads,
+//                       d = 128, bfloat16) behind 8150 positions take 570 us, 890 TFLOP/s, the
+//                       matrix cores busy 42% of the cycles; 2 x 4096 rows of 12 heads (d = 64)
+//                       behind 4096 take 179 us, 590 TFLOP/s (twice the exponentials per
+//                       product); float32, 2048 rows of 4 heads behind 2048, 79 us, 64 TFLOP/s.
 //   paged_short_kernel  the rows of all query heads of a key head, where they are at most
 //                       16 in a sequence (single tokens above all): the waves take different
 //                       pages of the same rows.  Bound by memory: a page is read once for
-//                       all query heads that share it.
+//                       all query heads that share it.  8 sequences of 4k to 64k positions, 12
+//                       heads, bfloat16: 51 us for 311 MB, 6.1 TB/s, what plain reads of such
+//                       pages reach.
 // The kept pages of all (rows, head) items, one after the other, are dealt in equal shares to
 // as many workgroups as the chip holds at a time, whatever lengths and heads they belong to:
 // paged_plan_kernel finds each item's pages, every workgroup adds up where its share lies,
@@ -27,8 +33,8 @@ namespace acp {
 namespace {
 
 constexpr int kShortRows = 16;    // rows of a short sequence: new tokens times query heads
-constexpr float kSlack = 8.f;     // a weight is at most 2^8
-constexpr double kFixedMax = 52.0;
+constexpr float kSlack = 8.f;     // a weight is at most 2^8 (2^2: chunks 10% slower, for 5% less error)
+constexpr double kFixedMax = 52.0;    // largest bound U that serves as reference (paged_long_kernel)
 
 __device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
@@ -136,7 +142,8 @@ struct RowBlock {
             l[qt] += y[j];
         }
     }
-    // acc += V^T P^T; v(dt, j): bf16 the lane's eight keys of column 16 dt + r (j unused),
+    // acc += V^T P^T, the weights rounded to T for the matrix cores (their sum l is not: the
+    // log-sum-exp keeps float32's precision, and O is off by what 2^-9 of a weight makes); v(dt, j): bf16 the lane's eight keys of column 16 dt + r (j unused),
     // float the key of element j
     template <typename F>
     __device__ __forceinline__ void add(const float (&p)[NQ][8], F v) {
@@ -930,7 +937,8 @@ struct GateDma {
     }
 };
 
-// Rows r = token * G + head of the group, r < 16, are the queries of every wave.
+// Rows r = token * G + head of the group, r < 16, are the queries of every wave.  A step's
+// operands are requested one step ahead; at d = 64 in bfloat16 two workgroups fit a CU.
 // gates_lds: the page's gates go through LDS (GateDma::bytes(G) more of it per wave), else each
 // lane loads those of its head and keys.
 template <typename T, int D>
@@ -1279,11 +1287,13 @@ struct Division {
     size_t bytes;
 };
 
+// (at least so many workgroups, so that a max_len that is too small still spreads the pages)
 constexpr int kLeastShares = 96;
 
 // A kernel's items, and their shares: `fit` workgroups (what the chip holds at a time), no
 // share under `least` pages.  Items that are many more, or have few pages, are not shared
-// out: at 8 items per workgroup the last ones to finish cost an eighth at most.
+// out: at 8 items per workgroup the last ones to finish cost an eighth at most (8400 items of
+// 10 to 20 pages 355 us, shared out 381; at 3000 items of 16 to 45 pages both take 242).
 void share_out(Work& w, int64_t items, int fit, int setup, int least, int64_t pages) {
     w.n = (int)items;
     w.least = least;
@@ -1303,6 +1313,8 @@ Division divide(const PagedArgs& a) {
     // (rows in equal parts that are long: no sequence is short)
     v.short_on = !v.long_on || (int64_t)a.N * a.max_new != a.T;
     v.long_above = v.short_on ? v.short_max : 0;
+    // (4 x 64 rows behind 4000, 12 heads of 64: 28 us at one, 32 at two; 2 x 4096 rows 179 at
+    // two, 241 at one)
     v.nq = a.max_new > 64 ? 2 : 1;
     const int rows = 64 * v.nq;
     auto take = [&](size_t n) {
@@ -1322,11 +1334,17 @@ Division divide(const PagedArgs& a) {
         v.lw.tiles = (int)((a.T + (int64_t)a.N * (rows - 1)) / rows);
         // workgroups at a time: by registers three per CU (d = 64, bfloat16) or by LDS two, one
         const int fit = 256 * (a.d * es == 128 ? 3 : a.d * es == 256 ? 2 : 1);
+        // taking up an item costs 9 of the faster pages of bfloat16 (8000 rows behind 8150 591 us,
+        // counted as 4 623, as 16 598; chunks beside single tokens 70, 73, 75), 2 of float32's
         share_out(v.lw, (int64_t)v.lw.tiles * a.H, fit, a.bf16 ? 9 : 2, a.bf16 ? 10 : 4, pages);
         place(v.lw, rows);
     }
     if (v.short_on) {
         v.sw.tiles = a.N;
+        // two workgroups per CU in bfloat16 (d = 128 holds one at a time: 16 tokens of 32 heads on 4
+        // key heads 103 us, with one per CU 105), one in float32 (8 tokens of 12 heads 59 us, with
+        // two 67); an item costs 7 pages (256 tokens 242 us, counted as 4 264; the 16 tokens 103,
+        // counted as 10 107)
         share_out(v.sw, (int64_t)a.N * a.Hk, a.bf16 ? 512 : 256, 7, 8, pages);
         place(v.sw, kShortRows);
     }
