@@ -148,7 +148,9 @@ acp_status acp_paged_append(const void* k, const int64_t* k_strides, const void*
  * j <= i of its sequence with logit q.k / sqrt(d) + c_i - c_j.  With ACP (eps > 0) page
  * n < i / 64 is left out where c_i - c_{64 n + 63} < delta, delta = -(2 U + log L_max - log eps),
  * U = gamma_q[h] gamma_k[h / (H / Hk)] sqrt(d) (App. E, App. F: the row-wise block test of
- * fox_attn_decode); eps = 0 leaves nothing out and gamma_q, gamma_k may be null.
+ * fox_attn_decode); eps = 0 leaves nothing out and gamma_q, gamma_k may be null.  The scales
+ * must bound the logits, |q.k| / sqrt(d) <= U up to rounding: U also keeps the weights in
+ * float32's range.
  * The entries of pages that no row keeps any more may be set to -1 (and the pages used anew):
  * with eps > 0 the search for a row's first kept page takes an entry out of range for a page
  * that the test leaves out, and with it the pages before it, and reports neither.  An entry
