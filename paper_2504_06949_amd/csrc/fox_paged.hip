@@ -107,8 +107,11 @@ struct RowBlock {
             }
         }
     }
-    // y - ref (log2 units, -inf: left out) -> weights; true if ref[qt] moved
-    __device__ __forceinline__ bool weights(int qt, float (&y)[8]) {
+    // y - ref (log2 units, -inf: left out) -> weights; true if ref[qt] moved.  again(y) forms
+    // y - ref anew from the products, in float32: formed with a ref far below, y has been rounded
+    // in proportion to its distance (1.7e-6 of a row's O where the first keys seen are forgotten).
+    template <typename F>
+    __device__ __forceinline__ bool weights(int qt, float (&y)[8], F again) {
         float mx = fmaxf(y[0], y[1]);
 #pragma unroll
         for (int j = 2; j < 8; j += 2) mx = fmaxf(fmaxf(mx, y[j]), y[j + 1]);
@@ -126,6 +129,7 @@ struct RowBlock {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) y[j] -= mx;
             }
+            if constexpr (!is_bf16<T>() || NQ == 1) again(y);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -760,6 +764,21 @@ void paged_long_kernel(PagedArgs, Work work, float kscale) {
             };
             if constexpr (kAhead) load_values();
             float p[NQ][8];
+            // weights of query subtile qt; form(qt, p): its y - ref
+            auto weigh = [&](int qt, auto form) __attribute__((always_inline)) {
+                if constexpr (kFixed) {
+                    blk.weights_fixed(qt, p[qt]);
+                } else {
+                    auto moved = [&]() __attribute__((always_inline)) {
+                        row[qt] = __builtin_fmaf(sm.rd[o0 + 16 * qt + r16].x, kLog2e, -blk.ref[qt]);
+                    };
+                    if (blk.weights(qt, p[qt], [&](float (&y)[8]) __attribute__((always_inline)) {
+                            moved();
+                            form(qt, y);
+                        }))
+                        moved();
+                }
+            };
             if constexpr (kMask) {
                 float2 kd[8], rd[NQ];
 #pragma unroll
@@ -769,33 +788,34 @@ void paged_long_kernel(PagedArgs, Work work, float kscale) {
                 // (held here: read where they are used, each read would stand in a branch of its own)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) asm volatile("" : "+v"(kd[j].x), "+v"(kd[j].y));
-#pragma unroll
-                for (int qt = 0; qt < NQ; ++qt) {
+                auto form = [&](int qt, float (&y)[8]) __attribute__((always_inline)) {
                     // keys up to `last` of the half
                     const int last = keep[qt] ? pos_of(qt) - 64 * n - 32 * ks : -1;
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         const float decay = (rd[qt].x - kd[j].x) + (rd[qt].y - kd[j].y);
-                        const float y = __builtin_fmaf(x[j >> 2][qt][j & 3], kscale,
+                        const float v = __builtin_fmaf(x[j >> 2][qt][j & 3], kscale,
                                                        __builtin_fmaf(decay, kLog2e, -blk.ref[qt]));
-                        p[qt][j] = key_of<T>(g, j) <= last ? y : -INFINITY;
+                        y[j] = key_of<T>(g, j) <= last ? v : -INFINITY;
                     }
-                }
+                };
+#pragma unroll
+                for (int qt = 0; qt < NQ; ++qt) form(qt, p[qt]);
+#pragma unroll
+                for (int qt = 0; qt < NQ; ++qt) weigh(qt, form);
             } else {
                 float kb[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) kb[j] = sm.kb[buf][32 * ks + key_of<T>(g, j)];
-#pragma unroll
-                for (int qt = 0; qt < NQ; ++qt)
+                auto form = [&](int qt, float (&y)[8]) __attribute__((always_inline)) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
-                        p[qt][j] = __builtin_fmaf(x[j >> 2][qt][j & 3], kscale, kFixed ? kb[j] : kb[j] + row[qt]);
-            }
+                        y[j] = __builtin_fmaf(x[j >> 2][qt][j & 3], kscale, kFixed ? kb[j] : kb[j] + row[qt]);
+                };
 #pragma unroll
-            for (int qt = 0; qt < NQ; ++qt) {
-                if constexpr (kFixed) blk.weights_fixed(qt, p[qt]);
-                else if (blk.weights(qt, p[qt]))
-                    row[qt] = __builtin_fmaf(sm.rd[o0 + 16 * qt + r16].x, kLog2e, -blk.ref[qt]);
+                for (int qt = 0; qt < NQ; ++qt) form(qt, p[qt]);
+#pragma unroll
+                for (int qt = 0; qt < NQ; ++qt) weigh(qt, form);
             }
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (!kAhead) load_values();
@@ -1110,15 +1130,18 @@ __global__ __launch_bounds__(256, is_bf16<T>() && D == 64 ? 2 : 1) void paged_sh
 #pragma unroll
         for (int ks = 0; ks < KH; ++ks) {
             float p[1][8];
+            auto form = [&](float (&y)[8]) __attribute__((always_inline)) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int key = 32 * (ks + hf) + key_of<T>(g, j);
-                const bool on = keep && 64 * n + key <= pi;
-                const float y = __builtin_fmaf(x[ks][j >> 2][0][j & 3], kscale,
-                                               __builtin_fmaf(decay[ks][j], kLog2e, -blk.ref[0]));
-                p[0][j] = on ? y : -INFINITY;
-            }
-            blk.weights(0, p[0]);
+                for (int j = 0; j < 8; ++j) {
+                    const int key = 32 * (ks + hf) + key_of<T>(g, j);
+                    const bool on = keep && 64 * n + key <= pi;
+                    const float v = __builtin_fmaf(x[ks][j >> 2][0][j & 3], kscale,
+                                                   __builtin_fmaf(decay[ks][j], kLog2e, -blk.ref[0]));
+                    y[j] = on ? v : -INFINITY;
+                }
+            };
+            form(p[0]);
+            blk.weights(0, p[0], form);
             blk.add(p, [&](int dt, int j) __attribute__((always_inline)) {
                 if constexpr (is_bf16<T>()) return tile_col8(sm.v[wave][buf], 32 * ks + 8 * g, 16 * dt, r16);
                 else return vc[dt][j];

@@ -485,3 +485,23 @@ def test_scales_on_both_sides_of_a_known_reference(d, scale, dtype):
     """U = scale^2 sqrt(d) above 32 (35 to 50) and above 52: the two ways in which the weights of
     a chunk are kept in float32's range."""
     serve(World([100, 1], [300, 200], 2, 1, d, dtype, seed=22, scale=scale, mu=(2.0, 7.0)))
+
+
+@pytest.mark.parametrize("new,past", [([1], [63]), ([40], [24]), ([100], [60])])
+def test_the_keys_that_count_come_after_forgotten_ones(new, past):
+    """float32, queries of zero, gates that forget e^-5 a position: what the softmax is first
+    scaled by is far below the row's own logit, 0.  Of a row i, keys i and i - 1 alone count
+    (e^-10 and less of the rest): the decays, |c_i - c_j| <= 6, are rounded with 6 e, their
+    logits with 4 e |logit| + 4 e, a power of two with 2 e, and sums of at most 16 + 8 terms, the
+    scales of four waves and the division with 40 e: 100 e covers lse, and O relative to max |v|."""
+    w = World(new, past, 16, 16, 64, F32, seed=23, mu=(-5.2, -4.8))
+    w.q = [torch.zeros_like(t) for t in w.q]
+    w.fill_past()
+    w.append()
+    for eps in (EPS, 0.0):
+        o, lse = w.attend(eps)
+        for h in range(16):
+            ro, _, rl, _ = w.reference(0, h, eps, 4096)
+            vmax = w.v[0][:, h].abs().max().double()
+            assert (lse[:, h].double() - rl).abs().max() <= 100 * E, (h, float((lse[:, h].double() - rl).abs().max() / E))
+            assert (o[:, h].double() - ro).abs().max() <= 100 * E * vmax, h
