@@ -487,15 +487,20 @@ def test_scales_on_both_sides_of_a_known_reference(d, scale, dtype):
     serve(World([100, 1], [300, 200], 2, 1, d, dtype, seed=22, scale=scale, mu=(2.0, 7.0)))
 
 
+@pytest.mark.parametrize("forget", [5.0, 20.0])
 @pytest.mark.parametrize("new,past", [([1], [63]), ([40], [24]), ([100], [60])])
-def test_the_keys_that_count_come_after_forgotten_ones(new, past):
-    """float32, queries of zero, gates that forget e^-5 a position: what the softmax is first
-    scaled by is far below the row's own logit, 0.  Of a row i, keys i and i - 1 alone count
-    (e^-10 and less of the rest): the decays, |c_i - c_j| <= 6, are rounded with 6 e, their
-    logits with 4 e |logit| + 4 e, a power of two with 2 e, and sums of at most 16 + 8 terms, the
-    scales of four waves and the division with 40 e: 100 e covers lse, and O relative to max |v|."""
-    w = World(new, past, 16, 16, 64, F32, seed=23, mu=(-5.2, -4.8))
+def test_the_keys_that_count_come_after_forgotten_ones(new, past, forget):
+    """float32, queries of one feature, gates that forget e^-5 or e^-20 a position: what the
+    softmax is first scaled by is far below the row's own logit, which is k_5, below 5.  Its own key
+    counts, and the one before with e^-5 times e^(k_5 - k_5') at most: a logit, one product and one
+    decay, is rounded with 4 e |logit| + 4 e <= 24 e, a decay with 6 e times its weight, a power of
+    two with 2 e, and sums of at most 16 + 8 terms, the scales of four waves and the division with
+    40 e: 100 e covers lse, and O relative to max |v|."""
+    w = World(new, past, 16, 16, 64, F32, seed=23, mu=(-forget - 0.2, -forget + 0.2))
     w.q = [torch.zeros_like(t) for t in w.q]
+    for t in w.q:
+        t[..., 5] = 8.0
+    assert max(float(k[..., 5].abs().max()) for k in w.k) < 5.0
     w.fill_past()
     w.append()
     for eps in (EPS, 0.0):
