@@ -108,8 +108,8 @@ struct RowBlock {
         }
     }
     // y - ref (log2 units, -inf: left out) -> weights; true if ref[qt] moved.  again(y) forms
-    // y - ref anew from the products, in float32: formed with a ref far below, y has been rounded
-    // in proportion to its distance (1.7e-6 of a row's O where the first keys seen are forgotten).
+    // y - ref anew from the products: formed with a ref far below, y has been rounded in
+    // proportion to its distance (2e-5 in the log-sum-exp where the first keys seen are forgotten).
     template <typename F>
     __device__ __forceinline__ bool weights(int qt, float (&y)[8], F again) {
         float mx = fmaxf(y[0], y[1]);
@@ -126,10 +126,8 @@ struct RowBlock {
                 l[qt] *= alpha;
 #pragma unroll
                 for (int dt = 0; dt < ND; ++dt) acc[qt][dt] *= alpha;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] -= mx;
             }
-            if constexpr (!is_bf16<T>() || NQ == 1) again(y);
+            again(y);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {

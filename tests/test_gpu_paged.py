@@ -487,16 +487,18 @@ def test_scales_on_both_sides_of_a_known_reference(d, scale, dtype):
     serve(World([100, 1], [300, 200], 2, 1, d, dtype, seed=22, scale=scale, mu=(2.0, 7.0)))
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("forget", [5.0, 20.0])
 @pytest.mark.parametrize("new,past", [([1], [63]), ([40], [24]), ([100], [60])])
-def test_the_keys_that_count_come_after_forgotten_ones(new, past, forget):
-    """float32, queries of one feature, gates that forget e^-5 or e^-20 a position: what the
+def test_the_keys_that_count_come_after_forgotten_ones(new, past, forget, dtype):
+    """Queries of one feature, gates that forget e^-5 or e^-20 a position: what the
     softmax is first scaled by is far below the row's own logit, which is k_5, below 5.  Its own key
     counts, and the one before with e^-5 times e^(k_5 - k_5') at most: a logit, one product and one
     decay, is rounded with 4 e |logit| + 4 e <= 24 e, a decay with 6 e times its weight, a power of
     two with 2 e, and sums of at most 16 + 8 terms, the scales of four waves and the division with
-    40 e: 100 e covers lse, and O relative to max |v|."""
-    w = World(new, past, 16, 16, 64, F32, seed=23, mu=(-forget - 0.2, -forget + 0.2))
+    40 e; the logits' bound as reference, 8, adds 20 e: 100 e covers lse, and O relative to max |v|
+    but for the weights' and its own rounding to bfloat16."""
+    w = World(new, past, 16, 16, 64, dtype, seed=23, mu=(-forget - 0.2, -forget + 0.2))
     w.q = [torch.zeros_like(t) for t in w.q]
     for t in w.q:
         t[..., 5] = 8.0
@@ -509,4 +511,4 @@ def test_the_keys_that_count_come_after_forgotten_ones(new, past, forget):
             ro, _, rl, _ = w.reference(0, h, eps, 4096)
             vmax = w.v[0][:, h].abs().max().double()
             assert (lse[:, h].double() - rl).abs().max() <= 100 * E, (h, float((lse[:, h].double() - rl).abs().max() / E))
-            assert (o[:, h].double() - ro).abs().max() <= 100 * E * vmax, h
+            assert (o[:, h].double() - ro).abs().max() <= (100 * E + (2.0 ** -7 if dtype == BF else 0.0)) * vmax, h
