@@ -652,7 +652,7 @@ void paged_long_kernel(PagedArgs, Work work, float kscale) {
     // The logits of a head lie in [-U, U] by ACP's bound, less a decay that a row's own key has
     // not.  A ref that leaves that key's weight at e^(-64) or more, and every weight at
     // e^(2 kFixedMax - 64) or less, need not be looked for (8000 rows of 16 heads behind 8150,
-    // d = 128: 580 us instead of 664).  Not in float32, where products that start at a term as
+    // d = 128: 580 us instead of 690).  Not in float32, where products that start at a term as
     // large as U lose bits that count (1.3e-6 instead of 2.6e-7 of O's size).
     const double u = readfirst_f64(head_bound(a, h));
     const bool fixed = is_bf16<T>() && u >= 0.0 && u <= kFixedMax;
