@@ -14,7 +14,10 @@ PyTorch's current stream of the tensors' device.  A serving step of a QK-normed 
     o, lse = cache.attend(q[0].transpose(0, 1), cu, past, table, max_new,
                           gamma_q=gq, gamma_k=gk, eps=eps, L_max=L_max)
 
-and of training: rms_norm, rope, then acp.fox_attention.
+and of training: rms_norm, rope, then acp.fox_attention.  Into a HIP graph record the calls
+without autograd (norm_forward, norm_backward, Rotary.forward and backward, append, attend): a
+backward() recorded while an eager graph of the same leaves is alive works on that graph's
+stream, which can end the process.
 """
 from __future__ import annotations
 
