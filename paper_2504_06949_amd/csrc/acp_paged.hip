@@ -23,6 +23,14 @@ constexpr int kFewTokens = 16;                       // summed one after the oth
 constexpr int kGateHeadsLong = 1, kGateHeadsShort = 4;
 static_assert(kWaves * kGateHeadsShort == 64, "a total per lane");
 
+// Flags of a log gate x and of the sum c that it leads to
+__device__ __forceinline__ int gate_flags(float x, double c) {
+    int f = !__builtin_isfinite(x) ? 2 : x > 0.0f ? 1 : 0;
+    const double size = __builtin_fabs(c);
+    if (size >= 0x1p32 && size < INFINITY) f |= size > 0x1.fffffep127 ? 6 : 4;
+    return f;
+}
+
 struct GateSmem {
     double total[2][kWaves * kGateHeadsShort];       // [head][wave] of the pages of a step, in turn
     int flags[kGateHeadsShort];
@@ -38,8 +46,8 @@ __device__ __forceinline__ void append_few_gates(const PagedArgs& a, int s, cons
 #pragma unroll 4
         for (int r = 0; r < q.n; ++r) {
             const float x = f[(int64_t)r * a.ft];
-            flags |= !__builtin_isfinite(x) ? 2 : x > 0.0f ? 1 : 0;
             c += (double)x;
+            flags |= gate_flags(x, c);
             const int pos = q.past + r, p = page_of(a, s, pos >> 6);
             if (p < 0) flags |= kFlagPage;
             else a.cp[((int64_t)p * a.H + h) * 64 + (pos & 63)] = c;
@@ -114,7 +122,6 @@ __device__ __forceinline__ void append_gates(const PagedArgs& a, int s, int h0, 
             double incl[kGateHeads];
 #pragma unroll
             for (int k = 0; k < kGateHeads; ++k) {
-                if (is_new) flags[k] |= !__builtin_isfinite(x[j][k]) ? 2 : x[j][k] > 0.0f ? 1 : 0;
                 incl[k] = wave_inclusive_scan_f64(is_new ? (double)x[j][k] : 0.0);
             }
             if (lane == 63)
@@ -131,8 +138,9 @@ __device__ __forceinline__ void append_gates(const PagedArgs& a, int s, int h0, 
 #pragma unroll
             for (int k = 0; k < kGateHeads; ++k) {
                 const double before = wave > 0 ? readlane_f64(tot, 16 * k + max(wave - 1, 0)) : 0.0;
-                if (is_new && p >= 0 && h0 + k < a.H)
-                    a.cp[((int64_t)p * a.H + h0 + k) * 64 + lane] = c[k] + (before + incl[k]);
+                const double sum = c[k] + (before + incl[k]);
+                if (is_new) flags[k] |= gate_flags(x[j][k], sum);
+                if (is_new && p >= 0 && h0 + k < a.H) a.cp[((int64_t)p * a.H + h0 + k) * 64 + lane] = sum;
                 c[k] += readlane_f64(tot, 16 * k + kWaves - 1);
             }
         }

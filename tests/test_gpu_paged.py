@@ -512,3 +512,38 @@ def test_the_keys_that_count_come_after_forgotten_ones(new, past, forget, dtype)
             vmax = w.v[0][:, h].abs().max().double()
             assert (lse[:, h].double() - rl).abs().max() <= 100 * E, (h, float((lse[:, h].double() - rl).abs().max() / E))
             assert (o[:, h].double() - ro).abs().max() <= (100 * E + (2.0 ** -7 if dtype == BF else 0.0)) * vmax, h
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("new,past", [([100], [100]), ([1], [150]), ([12], [100]), ([3, 90], [110, 0])])
+@pytest.mark.parametrize("gate", [-1e4, -1e7, float(torch.finfo(torch.float32).min)])
+def test_a_gate_that_forgets_everything(new, past, dtype, gate):
+    """As between two texts: no row after it attends to a position before it.  A gate whose sum
+    leaves float64 too few bits for the gates after it is reported."""
+    w = World(new, past, 4, 2, 64, dtype, seed=24, mu=(2.0, 7.0))
+    for s in range(len(new)):
+        w.f[s][past[s] + new[s] // 2 if new[s] > 1 else 70] = gate
+    w.c = [torch.cumsum(f.double(), 0) for f in w.f]
+    w.fill_past()
+    flags = torch.zeros((len(new), 4), dtype=torch.int32, device="cuda")
+    w.append(flags=flags)
+    w.check_pages()
+    far = gate < -2.0 ** 32
+    assert (flags == (4 if far else 0)).all()
+    for eps in (EPS, 0.0):
+        w.check(*w.attend(eps), eps)
+
+
+def test_sums_that_leave_the_range_are_reported():
+    low = float(torch.finfo(torch.float32).min)
+    for new in ([9], [100]):
+        w = World(new, [3], 2, 2, 64, BF, seed=25)
+        w.f[0][5, 0], w.f[0][8, 0] = low, low            # c = -6.8e38
+        w.f[0][6, 1] = -2.0 ** 31
+        w.fill_past()
+        flags = torch.zeros((1, 2), dtype=torch.int32, device="cuda")
+        w.append(flags=flags)
+        assert flags.tolist() == [[6, 0]]
+        w.f[0][7, 1] = -2.0 ** 31
+        w.append(flags=flags)
+        assert flags.tolist() == [[6, 4]]
