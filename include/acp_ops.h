@@ -164,7 +164,8 @@ acp_status acp_paged_append(const void* k, const int64_t* k_strides, const void*
  *        more than max_new may be left as they are (flag bit 7 says they were); max_len is a
  *        hint that any value may have.
  *   out: O [T, H, d] dt, lse [T, H] float, contiguous; a row all of whose keys were
- *        left out by bad pages gets O = 0, lse = -inf.
+ *        left out by bad pages gets O = 0, lse = -inf; c_i counts as 0 where the row's own
+ *        page is bad.
  *   ws : acp_paged_workspace_size() bytes.
  * A value that is not finite reaches the rows that attend to its position, and only them.
  * Flag bit 3: a negative or not finite gamma. */

@@ -285,7 +285,7 @@ struct alignas(32) Item {
     int p0;            // position of the first
     int len;           // of the sequence, its new rows included
     int lo, pages;
-    int pad;
+    int own;           // long: the pages of its rows are there (else c_i, where one is bad, is 0)
 };
 // What a workgroup found at the start of its share: where the first page of it that another
 // share has pages in front of lies, for the merge (item -1: none, or an earlier share says so)
@@ -347,6 +347,8 @@ __device__ __forceinline__ Item long_item(const PagedArgs& a, int id, int tiles,
     it.lo = first_page(a, s, h, it.p0 >> 6, readfirst_f64(gate_at(a, s, h, it.p0)),
                        readfirst_f64(head_delta(a, h)), lane);
     it.pages = page_count(a, it.lo, it.p0 + it.n - 1);
+    const int p = (it.p0 >> 6) + lane;
+    it.own = __all(p > (it.p0 + it.n - 1) >> 6 || page_of(a, s, p) >= 0);
     if (((it.p0 + it.n - 1) >> 6) >= a.W) report(a, s, h, lane);
     return it;
 }
@@ -487,7 +489,7 @@ __device__ __forceinline__ bool next_item(const Work& w, Share& sh, const Item& 
 __device__ __forceinline__ Item item_at(const Work& w, int i) {
     const Item t = w.items[i];
     auto u = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
-    return Item{u(t.s), u(t.t0), u(t.n), u(t.p0), u(t.len), u(t.lo), u(t.pages), 0};
+    return Item{u(t.s), u(t.t0), u(t.n), u(t.p0), u(t.len), u(t.lo), u(t.pages), u(t.own)};
 }
 
 // Page numbers of 64 consecutive pages, one per lane
@@ -655,7 +657,7 @@ void paged_long_kernel(PagedArgs, Work work, float kscale) {
     // d = 128: 580 us instead of 690).  Not in float32, where products that start at a term as
     // large as U lose bits that count (1.3e-6 instead of 2.6e-7 of O's size).
     const double u = readfirst_f64(head_bound(a, h));
-    const bool fixed = is_bf16<T>() && u >= 0.0 && u <= kFixedMax;
+    const bool fixed = is_bf16<T>() && it.own && u >= 0.0 && u <= kFixedMax;
     const float known = fixed ? (float)fmin(u, 64.0 - u) * kLog2e : 0.f;
     if (fixed) {
 #pragma unroll

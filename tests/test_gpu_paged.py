@@ -547,3 +547,27 @@ def test_sums_that_leave_the_range_are_reported():
         w.f[0][7, 1] = -2.0 ** 31
         w.append(flags=flags)
         assert flags.tolist() == [[6, 4]]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_rows_whose_own_page_is_bad(dtype):
+    """They attend to the pages that the tile's first row keeps, with c_i = 0: logits far above
+    the scales' bound.  Weights and O are off by 2^-8 and 2^-9 of max |v| in bfloat16, float32's
+    logits, of at most 200, by 1000 e."""
+    w = World([80], [300], 3, 3, 64, dtype, seed=26, mu=(0.3, 0.6))
+    w.fill_past()
+    w.append()
+    w.table[0, 5] = -1                                   # positions 320 to 383
+    flags = torch.zeros((1, 3), dtype=torch.int32, device="cuda")
+    o, lse = w.attend(flags=flags)
+    assert (flags == ops.FLAG_BAD_PAGE).all() and torch.isfinite(lse).all()
+    for h in range(3):
+        c, k, v = w.c[0][:, h], w.k[0][:, h].double(), w.v[0][:, h].double()
+        assert float(c[300]) < -90.0
+        delta = -(2 * 8.0 + math.log(4096) + 10.0)
+        lo = next(n for n in range(5) if n == 4 or c[300] - c[64 * n + 63] >= delta)
+        x = w.q[0][320:, h].double() @ k[64 * lo:320].t() / 8 - c[None, 64 * lo:320]
+        p = torch.softmax(x, 1)
+        lim = (2.0 ** -7 if dtype == BF else 1000 * E) * float(v.abs().max())
+        assert (o[20:, h].double() - p @ v[64 * lo:320]).abs().max() <= lim, h
+        assert (lse[20:, h].double() - torch.logsumexp(x, 1)).abs().max() <= 1000 * E * 200, h
