@@ -216,14 +216,11 @@ __device__ __forceinline__ void add_marks(f32x4 (&acc)[D / 16], const unsigned (
 // The sequence and the tile of `rows` tokens in it that global tile number `tile` is, among
 // the sequences of n tokens, lo < n <= hi; false when there are fewer tiles.
 __device__ __forceinline__ bool locate(const PagedArgs& a, int tile, int rows, int lo, int hi, int lane,
-                                       int& seq, int& local) {
+                                       int& seq, int& local, Seq& found) {
     int before = 0;
     for (int base = 0; base < a.N; base += 64) {
-        int t = 0;
-        if (base + lane < a.N) {
-            const Seq q = seq_of(a, base + lane);
-            if (q.n > lo && q.n <= hi) t = (q.n + rows - 1) / rows;
-        }
+        const Seq q = seq_of(a, min(base + lane, a.N - 1));
+        const int t = base + lane < a.N && q.n > lo && q.n <= hi ? (q.n + rows - 1) / rows : 0;
         int incl = t;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -235,6 +232,8 @@ __device__ __forceinline__ bool locate(const PagedArgs& a, int tile, int rows, i
             const int f = __builtin_ctzll(past);
             seq = __builtin_amdgcn_readfirstlane(base + f);
             local = __builtin_amdgcn_readfirstlane(tile - before - (__shfl(incl, f) - __shfl(t, f)));
+            auto of = [&](int v) { return __builtin_amdgcn_readlane(v, f); };
+            found = Seq{of(q.row0), of(q.n), of(q.past)};
             return true;
         }
         before += __shfl(incl, 63);
@@ -252,26 +251,34 @@ __device__ __forceinline__ double head_delta(const PagedArgs& a, int h) {
     return -(2.0 * head_bound(a, h) + a.log_lmax_over_eps);
 }
 
-// First page that the row at page nd with cumulative gate ci keeps: the test grows with the
-// page, and 64 pages are probed at a time.  A page that is not in the cache counts as left
-// out (it may have been dropped).
-__device__ __forceinline__ int first_page(const PagedArgs& a, int s, int h, int nd, double ci, double delta,
-                                          int lane) {
-    if (delta == -INFINITY) return 0;
-    int lo = 0, hi = nd;                    // the answer lies in [lo, hi]; hi is kept
+// First page that the row at position pos keeps: the test grows with the page, and 64 pages are
+// probed at a time, the first ones while the row's own gate is on its way.  A page that is not in
+// the cache counts as left out (it may have been dropped).
+__device__ __forceinline__ int first_page(const PagedArgs& a, int s, int h, int pos, int lane) {
+    if (a.gamma_q == nullptr || a.W == 0) return 0;
+    // (loads without a branch, so that they are asked for together)
+    const int* table = a.table + (int64_t)s * a.W;
+    auto entry = [&](int n) { return table[min(n, a.W - 1)]; };
+    auto page = [&](int e, int n) { return n < a.W && e >= 0 && e < a.P ? e : -1; };
+    auto gate = [&](int p, int slot) { return gates_of(a, max(p, 0), h)[slot]; };
+    int lo = 0, hi = pos >> 6;              // the answer lies in [lo, hi]; hi is kept
+    int step = (hi + 63) / 64, n = lane * step;
+    const int own_e = entry(hi), probe = entry(n);
+    const int own = page(own_e, hi);
+    int p = page(probe, n);
+    const double own_c = gate(own, pos & 63);
+    double end = gate(p, 63);
+    const double delta = head_delta(a, h), ci = own < 0 ? 0.0 : own_c;
     while (lo < hi) {
-        const int step = (hi - lo + 63) / 64;
-        const int n = lo + lane * step;
-        bool keep = true;
-        if (n < hi) {
-            const int p = page_of(a, s, n);
-            keep = p >= 0 && ci - gates_of(a, p, h)[63] >= delta;
-        }
-        const unsigned long long k = __ballot(keep);
+        const unsigned long long k = __ballot(n >= hi || (p >= 0 && ci - end >= delta));
         const int f = k ? __builtin_ctzll(k) : 64;
         const int top = min(lo + f * step, hi);
         if (f > 0) lo = min(lo + (f - 1) * step + 1, top);
         hi = top;
+        step = (hi - lo + 63) / 64;
+        n = lo + lane * step;
+        p = page(entry(n), n);
+        end = gate(p, 63);
     }
     return lo;
 }
@@ -336,16 +343,15 @@ __device__ __forceinline__ Item long_item(const PagedArgs& a, int id, int tiles,
     const int G = a.H / a.Hk, rest = id - id / (tiles * G) * tiles * G;
     Item it{-1, 0, 0, 0, 0, 0, 0, 0};
     int s, tile;
+    Seq q;
     // (the last tiles of a sequence have the most pages: they go first)
-    if (!locate(a, tiles - 1 - rest / G, kRows, short_max, 0x7fffffff, lane, s, tile)) return it;
-    const Seq q = seq_of(a, s);
+    if (!locate(a, tiles - 1 - rest / G, kRows, short_max, 0x7fffffff, lane, s, tile, q)) return it;
     it.s = s;
     it.t0 = q.row0 + tile * kRows;
     it.n = min(kRows, q.n - tile * kRows);
     it.p0 = q.past + tile * kRows;
     it.len = q.past + q.n;
-    it.lo = first_page(a, s, h, it.p0 >> 6, readfirst_f64(gate_at(a, s, h, it.p0)),
-                       readfirst_f64(head_delta(a, h)), lane);
+    it.lo = first_page(a, s, h, it.p0, lane);
     it.pages = page_count(a, it.lo, it.p0 + it.n - 1);
     const int p = (it.p0 >> 6) + lane;
     it.own = __all(p > (it.p0 + it.n - 1) >> 6 || page_of(a, s, p) >= 0);
@@ -394,13 +400,12 @@ __global__ __launch_bounds__(512) void paged_plan_kernel(PagedArgs a, Work lw, W
     const int hk = min(id / sw.tiles, a.Hk - 1);
     Item it{-1, 0, 0, 0, 0, 0, 0, 0};
     int s, tile;
-    if (id < sw.n && locate(a, id - hk * sw.tiles, short_max, 0, short_max, lane, s, tile)) {
-        const Seq q = seq_of(a, s);
+    Seq q;
+    if (id < sw.n && locate(a, id - hk * sw.tiles, short_max, 0, short_max, lane, s, tile, q)) {
         it = Item{s, q.row0, q.n, q.past, q.past + q.n, 0, 0, 0};
         for (int k = w; k < G; k += short_waves) {
             const int h = hk * G + k;
-            const int f = first_page(a, s, h, q.past >> 6, readfirst_f64(gate_at(a, s, h, q.past)),
-                                     readfirst_f64(head_delta(a, h)), lane);
+            const int f = first_page(a, s, h, q.past, lane);
             if (lane == 0) first[slot][k] = f;
             if (((it.len - 1) >> 6) >= a.W) report(a, s, h, lane);
         }
