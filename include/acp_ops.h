@@ -134,8 +134,9 @@ acp_status acp_paged_offsets(int P, int H, int Hk, int d, acp_dtype dt, acp_page
 /* Stores T new rows: keys and values [T, Hk, d] dt (strided, 16-byte aligned rows) into
  * their slots, and the cumulative gates from log_f [T, H] float (strided) on top of
  * c at position past - 1.  Storing the same rows at the same positions again leaves the
- * same pages.  Flag bit 0: some log f > 0; bit 1: not finite, or c leaves the float32 range;
- * bit 2: some |c| reaches 2^32, where float64 holds the differences of later gates to 2^-20
+ * same pages.  Flag bit 0: some log f > 0; bit 1: not finite, or c of a new position is not finite
+ * or outside the float32 range (a bad gate of an earlier call stays in every later sum);
+ * bit 2: some finite |c| reaches 2^32, where float64 holds the differences of later gates to 2^-20
  * and less (a gate of the type's lowest value takes all their bits: the positions after it
  * no longer forget).
  * Two sequences of one call must not store to the same page. */

@@ -23,11 +23,13 @@ constexpr int kFewTokens = 16;                       // summed one after the oth
 constexpr int kGateHeadsLong = 1, kGateHeadsShort = 4;
 static_assert(kWaves * kGateHeadsShort == 64, "a total per lane");
 
-// Flags of a log gate x and of the sum c that it leads to
+// Flags of a log gate x and of the sum c that it leads to (which may hold the infinity or NaN of
+// a gate of an earlier call)
 __device__ __forceinline__ int gate_flags(float x, double c) {
     int f = !__builtin_isfinite(x) ? 2 : x > 0.0f ? 1 : 0;
     const double size = __builtin_fabs(c);
-    if (size >= 0x1p32 && size < INFINITY) f |= size > 0x1.fffffep127 ? 6 : 4;
+    if (!(size <= 0x1.fffffep127)) f |= 2;
+    if (size >= 0x1p32 && size < INFINITY) f |= 4;
     return f;
 }
 
