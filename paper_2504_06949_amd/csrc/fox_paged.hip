@@ -683,7 +683,9 @@ void paged_long_kernel(PagedArgs, Work work, float kscale) {
         row[qt] = hi * kLog2e;
     }
     const double c_first = readfirst_f64(gate(w0));
-    const double c_tile_last = readfirst_f64(gate(p1));
+    // (NaN, no page is whole: where a row's own page is bad, the last row's gate says nothing of the
+    // others', and R may be far from these, so that it takes both floats of c_i - R and c_j - R)
+    const double c_tile_last = it.own ? readfirst_f64(gate(p1)) : __builtin_nan("");
 
     PageDma<T, D> dma;
     dma.init(wave, lane);

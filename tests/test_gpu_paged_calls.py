@@ -41,3 +41,86 @@ def test_a_sum_of_gates_that_is_not_finite_stays_reported(n, gate):
         cache.append(kv, kv, f, ints(0, rows), ints(at), table, flags=flags)
         assert flags.tolist() == [[0, 2, 0, 0, 2]], call
         at += rows
+
+
+# ---- rows whose own page is bad -----------------------------------------------------------
+
+def check_with_bad_pages(w, o, lse, bad, eps, rows, L_max=4096):
+    """O and lse of the given rows of sequence 0 where the pages `bad` are not in the cache: their keys are left out, and
+    c_i is 0 for a row on one.  Tolerances as in World.reference."""
+    p0, L = w.past[0], w.past[0] + w.new[0]
+    j = torch.arange(L, device="cuda")
+    i = j[p0:, None]
+    here = torch.ones(L // 64 + 1, dtype=torch.bool, device="cuda")
+    here[list(bad)] = False
+    here = here[j // 64]
+    wt = 2.0 ** -8 if w.dtype == BF else 0.0
+    half = torch.finfo(w.dtype).eps / 2
+    for h in range(w.H):
+        hk = h // (w.H // w.Hk)
+        q, k, v = w.q[0][p0:, h].double(), w.k[0][:, hk].double(), w.v[0][:, hk].double()
+        c = w.c[0][:, h]
+        decay = torch.where(here[p0:], c[p0:], 0.0)[:, None] - c[None]
+        seen = (j[None] <= i) & here[None]
+        if eps > 0:
+            delta = -(2 * float(w.gq[h].double() * w.gk[hk].double()) * math.sqrt(w.d) + math.log(L_max) - math.log(eps))
+            last = (j // 64 * 64 + 63).clamp(max=L - 1)
+            seen &= (j // 64)[None] == i // 64
+            seen |= (j[None] // 64 < i // 64) & here[None] & (decay.gather(1, last[None].expand_as(decay)) >= delta)
+        x = torch.where(seen, q @ k.t() / math.sqrt(w.d) + decay, -math.inf)
+        top = x.amax(1, keepdim=True)
+        p = torch.exp(x - top)
+        tot = p.sum(1, keepdim=True)
+        p = p / tot
+        t = E * ((w.d / 4 + 8) * (q.abs() @ k.abs().t() / math.sqrt(w.d) + decay.abs()) + 8 + 2 * (top - x))
+        pt = torch.where(seen, p * (t + wt + 200 * E), 0.0)
+        fin = torch.isfinite(v)
+        v0 = torch.where(fin, v, 0.0)
+        ro = p @ v0
+        to = pt @ v0.abs() + pt.sum(1)[:, None] * ro.abs() + 4 * E * ro.abs() + half * ro.abs()
+        reached = (seen.double() @ (~fin).double()) > 0          # a value that is not finite is seen
+        rl = (top + tot.log())[:, 0]
+        tl = torch.where(seen, p * (t + 200 * E), 0.0).sum(1) + 8 * E * (rl.abs() + 1)
+        go, gl = o[rows, h].double(), lse[rows, h].double()
+        ro, to, reached, rl, tl = (x[rows] for x in (ro, to, reached, rl, tl))
+        assert torch.equal(torch.isfinite(go), ~reached), (h, "which are finite")
+        assert ((go - ro).abs() / to)[~reached].max() <= 1, (h, "O", float(((go - ro).abs() / to)[~reached].max()))
+        assert ((gl - rl).abs() / tl).max() <= 1, (h, "lse", float(((gl - rl).abs() / tl).max()))
+
+
+def bad_page_world(new, past, bad, G, d, dtype, strong):
+    """Gates behind one that makes |c| 1e5.  Strong: they leave out all but a page or two, and there is a NaN
+    and an infinity in pages that rows with their own gate leave out, and c_i = 0 does not.  Weak: every
+    page counts for every row."""
+    w = World([new], [past], 2 * G, 2, d, dtype, seed=30, mu=(0.3, 0.6) if strong else (6.0, 9.0))
+    w.f[0][5] = -1e5
+    w.c = [torch.cumsum(f.double(), 0) for f in w.f]
+    if strong:
+        w.v[0][20, :, 7] = float("nan")
+        w.v[0][70, :, 9] = float("inf")
+    w.fill_past()
+    w.append()
+    for n in bad:
+        w.table[0, n] = (-1, w.P)[n % 2]
+    return w
+
+
+BAD_TILES = [(128, 300, [4]), (128, 300, [5]), (128, 300, [6]), (128, 300, [4, 6]),     # tiles of 128 rows
+             (60, 300, [4]), (60, 300, [5]), (200, 290, [6]),                           # of 64, two tiles
+             (16, 310, [4]), (16, 310, [5]), (3, 318, [5])]                             # few rows
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("new,past,bad", BAD_TILES)
+def test_good_rows_beside_rows_whose_own_page_is_bad(new, past, bad, dtype):
+    for G, d, strong in ((1, 64, True), (2, 128, True), (1, 64, False), (2, 128, False)):
+        print(f"case: own page bad new={new} past={past} bad={bad} G={G} d={d} strong={strong} {dtype}", flush=True)
+        w = bad_page_world(new, past, bad, G, d, dtype, strong)
+        good = torch.tensor([(past + r) // 64 not in bad for r in range(new)], device="cuda")
+        flags = torch.zeros((1, w.H), dtype=torch.int32, device="cuda")
+        for eps in (EPS, 0.0):
+            o, lse = w.attend(eps, flags=flags)
+            assert (flags == ops.FLAG_BAD_PAGE).all()
+            if good.any():
+                assert torch.isfinite(o[good]).all() or (eps == 0.0 and strong)
+                check_with_bad_pages(w, o, lse, bad, eps, good)
