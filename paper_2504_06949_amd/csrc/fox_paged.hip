@@ -283,6 +283,19 @@ __device__ __forceinline__ int first_page(const PagedArgs& a, int s, int h, int 
     return lo;
 }
 
+// First page that any of the rows at positions p0 .. p1 of a tile keeps: the first row's, and where a
+// row's own page is not in the cache (c_i counts as 0 there, which keeps more) that row's.  own: all are there.
+__device__ __forceinline__ int first_of_tile(const PagedArgs& a, int s, int h, int p0, int p1, int lane, bool& own) {
+    // (a tile's rows lie in three pages at most; their entries are asked for before the search)
+    const int n = (p0 >> 6) + lane, p = page_of(a, s, min(n, p1 >> 6));
+    int lo = first_page(a, s, h, p0, lane);
+    unsigned long long bad = __ballot(n <= p1 >> 6 && p < 0);
+    own = bad == 0;
+    for (; bad; bad &= bad - 1)
+        lo = min(lo, first_page(a, s, h, max(p0, ((p0 >> 6) + (int)__builtin_ctzll(bad)) << 6), lane));
+    return lo;
+}
+
 // ---- items and shares ------------------------------------------------------------------
 // An item: rows of a sequence that one head (short: one group of heads) takes over the pages
 // lo .. lo + pages - 1.
@@ -351,10 +364,10 @@ __device__ __forceinline__ Item long_item(const PagedArgs& a, int id, int tiles,
     it.n = min(kRows, q.n - tile * kRows);
     it.p0 = q.past + tile * kRows;
     it.len = q.past + q.n;
-    it.lo = first_page(a, s, h, it.p0, lane);
+    bool own;
+    it.lo = first_of_tile(a, s, h, it.p0, it.p0 + it.n - 1, lane, own);
+    it.own = own;
     it.pages = page_count(a, it.lo, it.p0 + it.n - 1);
-    const int p = (it.p0 >> 6) + lane;
-    it.own = __all(p > (it.p0 + it.n - 1) >> 6 || page_of(a, s, p) >= 0);
     if (((it.p0 + it.n - 1) >> 6) >= a.W) report(a, s, h, lane);
     return it;
 }
@@ -375,7 +388,7 @@ __device__ __forceinline__ void empty_row(const PagedArgs& a, int t, int h, int 
 
 // The items of both kernels, by workgroups of 8 waves: a wave per long item, and per head of
 // a short one (8 of them at a time), whose first page is the first that any head of the group
-// keeps for the first token.
+// keeps for any token.
 template <typename T, int kRows>
 __global__ __launch_bounds__(512) void paged_plan_kernel(PagedArgs a, Work lw, Work sw, int short_max,
                                                          int long_above, int short_waves) {
@@ -405,7 +418,8 @@ __global__ __launch_bounds__(512) void paged_plan_kernel(PagedArgs a, Work lw, W
         it = Item{s, q.row0, q.n, q.past, q.past + q.n, 0, 0, 0};
         for (int k = w; k < G; k += short_waves) {
             const int h = hk * G + k;
-            const int f = first_page(a, s, h, q.past, lane);
+            bool own;
+            const int f = first_of_tile(a, s, h, q.past, it.len - 1, lane, own);
             if (lane == 0) first[slot][k] = f;
             if (((it.len - 1) >> 6) >= a.W) report(a, s, h, lane);
         }
@@ -682,9 +696,10 @@ void paged_long_kernel(PagedArgs, Work work, float kscale) {
         sm.rd[i] = make_float2(hi, (float)(r - (double)hi));
         row[qt] = hi * kLog2e;
     }
-    const double c_first = readfirst_f64(gate(w0));
-    // (NaN, no page is whole: where a row's own page is bad, the last row's gate says nothing of the
-    // others', and R may be far from these, so that it takes both floats of c_i - R and c_j - R)
+    // Where a row's own page is bad, one row's gate says nothing of another's: for the wave no page
+    // is left out (infinity), and for the tile none is whole (NaN; R may be far from the others'
+    // gates then, so that it takes both floats of c_i - R and c_j - R)
+    const double c_first = it.own ? readfirst_f64(gate(w0)) : INFINITY;
     const double c_tile_last = it.own ? readfirst_f64(gate(p1)) : __builtin_nan("");
 
     PageDma<T, D> dma;

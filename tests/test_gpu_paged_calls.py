@@ -124,3 +124,33 @@ def test_good_rows_beside_rows_whose_own_page_is_bad(new, past, bad, dtype):
             if good.any():
                 assert torch.isfinite(o[good]).all() or (eps == 0.0 and strong)
                 check_with_bad_pages(w, o, lse, bad, eps, good)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("new,past,bad", BAD_TILES)
+def test_rows_whose_own_page_is_bad_whatever_their_neighbours_keep(new, past, bad, dtype):
+    """With c_i = 0 they leave out no page, also where the rows before them in the tile do: a value that is
+    not finite reaches them from any page."""
+    for G, d in ((1, 64), (2, 128)):
+        print(f"case: own page bad, rows new={new} past={past} bad={bad} G={G} d={d} {dtype}", flush=True)
+        w = bad_page_world(new, past, bad, G, d, dtype, True)
+        rows = torch.tensor([(past + r) // 64 in bad for r in range(new)], device="cuda")
+        for eps in (EPS, 0.0):
+            o, lse = w.attend(eps)
+            assert not torch.isfinite(o[rows][:, :, [7, 9]]).any()
+            check_with_bad_pages(w, o, lse, bad, eps, rows)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("new,past", [(128, 12300), (9, 12345)])
+def test_dropped_pages_in_front_of_rows_whose_own_page_is_bad(new, past, dtype):
+    """Pages that nobody keeps may be gone, hundreds of them: a row on a bad page starts behind them."""
+    w = World([new], [past], 2, 2, 64, dtype, seed=38, mu=(0.0, 1.0))
+    w.fill_past()
+    w.append()
+    bad = [past // 64 + 1]
+    gone = list(range(130))
+    w.table[0, gone + bad] = -1
+    o, lse = w.attend()
+    for rows in ([r for r in range(new) if (past + r) // 64 not in bad], [r for r in range(new) if (past + r) // 64 in bad]):
+        check_with_bad_pages(w, o, lse, bad + gone, EPS, torch.tensor(rows, device="cuda"))
