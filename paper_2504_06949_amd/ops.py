@@ -211,6 +211,8 @@ def norm_backward(dy, x, weight, mean, rstd, bias: bool = False):
     B, H, L, n = x4.shape
     dy4 = dy4.view(x4.shape) if dy4.dim() != 4 else dy4
     dx4 = torch.empty_like(x4)
+    if dx4.stride(3) != 1 and n > 1:         # (x's rows share features: no order of the axes to take over)
+        dx4 = x4.new_empty(x4.shape)
     dw = x.new_empty(weight.shape, dtype=torch.float32)
     db = torch.empty_like(dw) if bias else None
     need = _sz(0)

@@ -257,3 +257,39 @@ def test_second_derivatives_are_refused():
     g, = torch.autograd.grad(ops.rms_norm(x, w).sum(), x, create_graph=True)
     with pytest.raises(RuntimeError):
         g.sum().backward()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("shape,strides", [
+    ((5, 64), (1, 1)), ((500, 64), (1, 1)), ((2, 3, 5, 64), (7, 1, 1, 1)), ((2, 3, 5, 8), (8, 1, 8, 1)),
+    ((2, 1, 5, 8), (1, 0, 4, 1)), ((3, 4, 64), (0, 16, 1)), ((2, 3, 5, 64), (0, 64, 0, 1)), ((4, 5, 1), (1, 1, 3))])
+def test_gradients_of_rows_that_share_features(shape, strides, dtype):
+    """Windows into one row and broadcast rows: the gradient is that of separate rows, in memory of its
+    own for each."""
+    g = torch.Generator(device="cuda").manual_seed(40)
+    flat = torch.randn(4096, generator=g, device="cuda").to(dtype)
+    x = torch.as_strided(flat, shape, strides)
+    n = shape[-1]
+    per_head = len(shape) == 4
+    w = 1.0 + 0.1 * torch.randn((shape[1], n) if per_head else (n,), generator=g, device="cuda")
+    dy = torch.randn(shape, generator=g, device="cuda").to(dtype)
+    for center in (False, True):
+        y, mean, rstd = ops.norm_forward(x, w, center=center)
+        want_y, want_mean, want_rstd = ops.norm_forward(x.contiguous(), w, center=center)
+        got = ops.norm_backward(dy, x, w, mean, rstd, bias=True)
+        want = ops.norm_backward(dy, x.contiguous(), w, want_mean, want_rstd, bias=True)
+        assert torch.equal(y, want_y) and torch.equal(rstd, want_rstd)
+        for a, b in zip(got, want):
+            assert a.shape == b.shape and torch.equal(a, b)
+    leaf = flat.clone().requires_grad_()
+    rows = torch.as_strided(leaf, shape, strides)
+    ops.rms_norm(rows, w).backward(dy)
+    dx = ops.norm_backward(dy, x.contiguous(), w, None, ops.norm_forward(x, w)[2])[0]
+    want = torch.zeros(4096, dtype=torch.float64, device="cuda")
+    at = torch.as_strided(torch.arange(4096, device="cuda"), shape, strides)
+    want.index_add_(0, at.reshape(-1), dx.double().reshape(-1))
+    parts = torch.zeros(4096, dtype=torch.float64, device="cuda")
+    parts.index_add_(0, at.reshape(-1), dx.double().abs().reshape(-1))
+    # (autograd adds up to `many` of them in dtype, each addition off by half a step of a partial sum)
+    many = int(torch.bincount(at.reshape(-1)).max())
+    assert ((leaf.grad.double() - want).abs() <= many * _half(dtype) * parts * 1.01).all()
