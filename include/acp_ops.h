@@ -179,6 +179,15 @@ acp_status fox_attn_paged(const void* q, const int64_t* q_strides, acp_dtype dt,
                           double eps, int64_t L_max, int max_new, int64_t max_len, void* O,
                           float* lse, int32_t* flags, void* ws, size_t ws_bytes, void* stream);
 
+/* The same, for outputs that hold nothing yet: the rows that fox_attn_paged leaves as they are (from
+ * cu[N] on, and of a sequence with more than max_new where it says so) get O = 0, lse = -inf. */
+acp_status fox_attn_paged_filled(const void* q, const int64_t* q_strides, acp_dtype dt, int T, int N,
+                                 int W, int P, int H, int Hk, int d, const int32_t* cu,
+                                 const int32_t* past, const int32_t* table, const void* cache,
+                                 size_t cache_bytes, const float* gamma_q, const float* gamma_k,
+                                 double eps, int64_t L_max, int max_new, int64_t max_len, void* O,
+                                 float* lse, int32_t* flags, void* ws, size_t ws_bytes, void* stream);
+
 /* Timing of these operators, as acp_timing_read() of the others: the same switch and
  * reset (acp_timing_enable, acp_timing_reset). */
 enum {
@@ -186,7 +195,7 @@ enum {
     ACP_OP_NORM_BWD = 1,    /* acp_norm_bwd, the weight's sum included   */
     ACP_OP_ROTARY = 2,
     ACP_OP_APPEND = 3,
-    ACP_OP_ATTEND = 4,      /* fox_attn_paged, the merge of parts included */
+    ACP_OP_ATTEND = 4,      /* fox_attn_paged(_filled), the merge of parts included */
     ACP_OP_COUNT = 5
 };
 typedef struct {

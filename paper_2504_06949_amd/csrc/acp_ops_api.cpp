@@ -137,6 +137,49 @@ acp_status check_division(int max_new, int64_t max_len) {
     return ACP_OK;
 }
 
+// fox_attn_paged; fill: and the rows that nothing attends for
+acp_status attend_paged(bool fill, const void* q, const int64_t* q_strides, acp_dtype dt, int T, int N, int W, int P,
+                        int H, int Hk, int d, const int32_t* cu, const int32_t* past, const int32_t* table,
+                        const void* cache, size_t cache_bytes, const float* gamma_q, const float* gamma_k,
+                        double eps, int64_t L_max, int max_new, int64_t max_len, void* O, float* lse,
+                        int32_t* flags, void* ws, size_t ws_bytes, void* stream) {
+    ACP_TRY(check_paged(P, H, Hk, d, dt));
+    ACP_TRY(check_call(T, N, W, H, cu, past, table));
+    ACP_TRY(check_cache(cache, cache_bytes, paged_layout(P, H, Hk, d, dt)));
+    ACP_TRY(check_division(max_new, max_len));
+    if (!std::isfinite(eps) || eps < 0.0 || eps >= 1.0) return set_error(ACP_EINVAL, "eps=%g outside [0, 1)", eps);
+    if (eps > 0.0) {
+        if (L_max < 1 || L_max > (INT64_C(1) << 31))
+            return set_error(ACP_EINVAL, "L_max=%lld outside [1, 2^31]", (long long)L_max);
+        ACP_TRY(check_ptr(gamma_q, "gamma_q", 4));
+        ACP_TRY(check_ptr(gamma_k, "gamma_k", 4));
+    }
+    if (flags) ACP_TRY(check_ptr(flags, "flags", 4));
+    acp::PagedArgs a = paged_args(dt, T, N, W, P, H, Hk, d, cu, past, table, const_cast<void*>(cache), flags);
+    ACP_TRY(get_packed(q_strides, H, d, dt, "q", &a.qt, &a.qh));
+    a.max_new = max_new; a.max_len = max_len;
+    if (T > 0) {
+        ACP_TRY(check_ptr(q, "q", 16));
+        ACP_TRY(check_ptr(O, "O", 16));
+        ACP_TRY(check_ptr(lse, "lse", 4));
+        const size_t need = acp::paged_workspace(a);
+        if (need > 0) {
+            ACP_TRY(check_ptr(ws, "ws", 16));
+            if (ws_bytes < need)
+                return set_error(ACP_EWORKSPACE, "workspace of %zu bytes, %zu needed", ws_bytes, need);
+        }
+    }
+    if (N == 0 && !(fill && T > 0)) return ok();
+    a.q = q;
+    a.gamma_q = eps > 0.0 ? gamma_q : nullptr;
+    a.gamma_k = eps > 0.0 ? gamma_k : nullptr;
+    a.log_lmax_over_eps = eps == 0.0 ? INFINITY : std::log((double)L_max) - std::log(eps);
+    a.fill = fill;
+    a.O = O; a.lse = lse;
+    a.part = (float*)ws;
+    return hip_status(acp::launch_paged_attend(a, (hipStream_t)stream), "fox_attn_paged launch");
+}
+
 }  // namespace
 
 extern "C" {
@@ -368,40 +411,18 @@ acp_status fox_attn_paged(const void* q, const int64_t* q_strides, acp_dtype dt,
                           const void* cache, size_t cache_bytes, const float* gamma_q, const float* gamma_k,
                           double eps, int64_t L_max, int max_new, int64_t max_len, void* O, float* lse,
                           int32_t* flags, void* ws, size_t ws_bytes, void* stream) {
-    ACP_TRY(check_paged(P, H, Hk, d, dt));
-    ACP_TRY(check_call(T, N, W, H, cu, past, table));
-    ACP_TRY(check_cache(cache, cache_bytes, paged_layout(P, H, Hk, d, dt)));
-    ACP_TRY(check_division(max_new, max_len));
-    if (!std::isfinite(eps) || eps < 0.0 || eps >= 1.0) return set_error(ACP_EINVAL, "eps=%g outside [0, 1)", eps);
-    if (eps > 0.0) {
-        if (L_max < 1 || L_max > (INT64_C(1) << 31))
-            return set_error(ACP_EINVAL, "L_max=%lld outside [1, 2^31]", (long long)L_max);
-        ACP_TRY(check_ptr(gamma_q, "gamma_q", 4));
-        ACP_TRY(check_ptr(gamma_k, "gamma_k", 4));
-    }
-    if (flags) ACP_TRY(check_ptr(flags, "flags", 4));
-    acp::PagedArgs a = paged_args(dt, T, N, W, P, H, Hk, d, cu, past, table, const_cast<void*>(cache), flags);
-    ACP_TRY(get_packed(q_strides, H, d, dt, "q", &a.qt, &a.qh));
-    a.max_new = max_new; a.max_len = max_len;
-    if (T > 0) {
-        ACP_TRY(check_ptr(q, "q", 16));
-        ACP_TRY(check_ptr(O, "O", 16));
-        ACP_TRY(check_ptr(lse, "lse", 4));
-        const size_t need = acp::paged_workspace(a);
-        if (need > 0) {
-            ACP_TRY(check_ptr(ws, "ws", 16));
-            if (ws_bytes < need)
-                return set_error(ACP_EWORKSPACE, "workspace of %zu bytes, %zu needed", ws_bytes, need);
-        }
-    }
-    if (N == 0) return ok();
-    a.q = q;
-    a.gamma_q = eps > 0.0 ? gamma_q : nullptr;
-    a.gamma_k = eps > 0.0 ? gamma_k : nullptr;
-    a.log_lmax_over_eps = eps == 0.0 ? INFINITY : std::log((double)L_max) - std::log(eps);
-    a.O = O; a.lse = lse;
-    a.part = (float*)ws;
-    return hip_status(acp::launch_paged_attend(a, (hipStream_t)stream), "fox_attn_paged launch");
+    return attend_paged(false, q, q_strides, dt, T, N, W, P, H, Hk, d, cu, past, table, cache, cache_bytes, gamma_q,
+                        gamma_k, eps, L_max, max_new, max_len, O, lse, flags, ws, ws_bytes, stream);
+}
+
+acp_status fox_attn_paged_filled(const void* q, const int64_t* q_strides, acp_dtype dt, int T, int N, int W,
+                                 int P, int H, int Hk, int d, const int32_t* cu, const int32_t* past,
+                                 const int32_t* table, const void* cache, size_t cache_bytes,
+                                 const float* gamma_q, const float* gamma_k, double eps, int64_t L_max,
+                                 int max_new, int64_t max_len, void* O, float* lse, int32_t* flags, void* ws,
+                                 size_t ws_bytes, void* stream) {
+    return attend_paged(true, q, q_strides, dt, T, N, W, P, H, Hk, d, cu, past, table, cache, cache_bytes, gamma_q,
+                        gamma_k, eps, L_max, max_new, max_len, O, lse, flags, ws, ws_bytes, stream);
 }
 
 }  // extern "C"

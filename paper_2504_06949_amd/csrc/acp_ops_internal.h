@@ -67,6 +67,7 @@ struct PagedArgs {
     const float* gamma_q;
     const float* gamma_k;
     double log_lmax_over_eps; // +inf for eps = 0
+    bool fill;                // rows that nothing attends for: O = 0, lse = -inf
     int max_new;
     int64_t max_len;
     void* O;

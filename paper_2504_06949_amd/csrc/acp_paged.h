@@ -23,6 +23,17 @@ __device__ __forceinline__ Seq seq_of(const PagedArgs& a, int s) {
     return q;
 }
 
+// The sequence that holds packed row t, or -1: the last one that starts at or before it
+__device__ __forceinline__ int sequence_of(const PagedArgs& a, int t) {
+    int lo = 0, hi = a.N;                             // first s with cu[s + 1] > t
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (a.cu[mid + 1] > t) hi = mid;
+        else lo = mid + 1;
+    }
+    return lo < a.N && a.cu[lo] <= t ? lo : -1;
+}
+
 // Page n of sequence s, or -1
 __device__ __forceinline__ int page_of(const PagedArgs& a, int s, int n) {
     if (n >= a.W) return -1;

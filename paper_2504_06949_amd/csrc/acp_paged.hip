@@ -159,17 +159,6 @@ __device__ __forceinline__ void append_gates(const PagedArgs& a, int s, int h0, 
         a.flags[(int64_t)s * a.H + h0 + threadIdx.x] = sm.flags[threadIdx.x];
 }
 
-// The sequence that holds packed row t, or -1: the last one that starts at or before it
-__device__ __forceinline__ int sequence_of(const PagedArgs& a, int t) {
-    int lo = 0, hi = a.N;                             // first s with cu[s + 1] > t
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (a.cu[mid + 1] > t) hi = mid;
-        else lo = mid + 1;
-    }
-    return lo < a.N && a.cu[lo] <= t ? lo : -1;
-}
-
 template <typename T>
 __device__ __forceinline__ void append_rows(const PagedArgs& a, int t0, int tokens, int64_t* slot) {
     constexpr int VEC = 16 / (int)sizeof(T);

@@ -386,15 +386,37 @@ __device__ __forceinline__ void empty_row(const PagedArgs& a, int t, int h, int 
     if (lane == 0) a.lse[row] = -INFINITY;
 }
 
+// Rows 64 i .. 64 i + 63 of the call, by a wave: those that no sequence brings, or one of more than
+// `limit` rows, become empty
+template <typename T>
+__device__ __forceinline__ void fill_rows(const PagedArgs& a, int i, int limit, int lane) {
+    const int t = 64 * i + lane;
+    bool on = true;
+    if (t < a.T) {
+        const int s = sequence_of(a, t);
+        on = s >= 0 && seq_of(a, s).n <= limit;
+    }
+    for (unsigned long long rows = __ballot(!on); rows; rows &= rows - 1) {
+        const int64_t row = (int64_t)(64 * i + (int)__builtin_ctzll(rows)) * a.H;
+        uint4* o = reinterpret_cast<uint4*>((T*)a.O + row * a.d);
+        for (int e = lane; e < a.H * a.d * (int)sizeof(T) / 16; e += 64) o[e] = make_uint4(0, 0, 0, 0);
+        for (int h = lane; h < a.H; h += 64) a.lse[row + h] = -INFINITY;
+    }
+}
+
 // The items of both kernels, by workgroups of 8 waves: a wave per long item, and per head of
 // a short one (8 of them at a time), whose first page is the first that any head of the group
-// keeps for any token.
+// keeps for any token.  The workgroups from fill_at on look after the rows that no item has.
 template <typename T, int kRows>
 __global__ __launch_bounds__(512) void paged_plan_kernel(PagedArgs a, Work lw, Work sw, int short_max,
-                                                         int long_above, int short_waves) {
+                                                         int long_above, int short_waves, int fill_at, int limit) {
     __shared__ int first[8][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int nl = (lw.n + 7) / 8, G = a.H / a.Hk;
+    if ((int)blockIdx.x >= fill_at) {
+        fill_rows<T>(a, (blockIdx.x - fill_at) * 8 + wave, limit, lane);
+        return;
+    }
     if ((int)blockIdx.x < nl) {
         const int id = blockIdx.x * 8 + wave;
         if (id >= lw.n) return;
@@ -1326,7 +1348,7 @@ __global__ __launch_bounds__(256) void paged_flags_kernel(PagedArgs a, int limit
 // How a call is divided.  Sequences of at most short_max new tokens go to the short kernel,
 // the others to the long one, tiles of 64 nq rows.
 struct Division {
-    int short_max, long_above, nq;
+    int short_max, long_above, nq, limit;     // limit: rows of a sequence that its kernels take
     bool short_on, long_on;
     Work lw, sw;       // offsets from the workspace in place of the pointers
     size_t bytes;
@@ -1354,7 +1376,10 @@ Division divide(const PagedArgs& a) {
     const int G = a.H / a.Hk, es = a.bf16 ? 2 : 4;
     v.short_max = kShortRows / G;
     const int64_t pages = (a.max_len + 63) / 64;
-    v.long_on = a.max_new > v.short_max;
+    v.long_on = a.N > 0 && a.max_new > v.short_max;
+    v.limit = v.long_on ? 0x7fffffff : v.short_max;
+    v.nq = 1;
+    if (a.N == 0) return v;
     // (rows in equal parts that are long: no sequence is short)
     v.short_on = !v.long_on || (int64_t)a.N * a.max_new != a.T;
     v.long_above = v.short_on ? v.short_max : 0;
@@ -1407,8 +1432,9 @@ void attend(const PagedArgs& a, const Division& v, hipStream_t s) {
         w->slots = (float*)((char*)a.part + (size_t)w->slots);
     }
     const int G = a.H / a.Hk, waves = G <= 1 ? 1 : G <= 2 ? 2 : G <= 4 ? 4 : 8;   // of a short item
-    hipLaunchKernelGGL((paged_plan_kernel<T, 64 * NQ>), dim3((lw.n + 7) / 8 + (sw.n * waves + 7) / 8), dim3(512), 0,
-                       s, a, lw, sw, v.short_max, v.long_above, waves);
+    const int fill_at = (lw.n + 7) / 8 + (sw.n * waves + 7) / 8, fill = a.fill ? (a.T + 511) / 512 : 0;
+    hipLaunchKernelGGL((paged_plan_kernel<T, 64 * NQ>), dim3(fill_at + fill), dim3(512), 0, s, a, lw, sw,
+                       v.short_max, v.long_above, waves, fill_at, v.limit);
     if (v.long_on)
         hipLaunchKernelGGL((paged_long_kernel<T, D, NQ>), dim3(lw.wgs), dim3(256), 0, s, a, lw, kscale);
     if (v.short_on) {
@@ -1435,9 +1461,9 @@ size_t paged_workspace(const PagedArgs& a) { return divide(a).bytes; }
 hipError_t launch_paged_attend(const PagedArgs& a, hipStream_t s) {
     trace_begin(ACP_K_COUNT + ACP_OP_ATTEND, s);
     const Division v = divide(a);
-    if (a.flags)
+    if (a.flags && a.N > 0)
         hipLaunchKernelGGL(paged_flags_kernel, dim3((unsigned)(((int64_t)a.N * a.H + 255) / 256)), dim3(256), 0,
-                           s, a, v.long_on ? 0x7fffffff : v.short_max);
+                           s, a, v.limit);
     if (a.T > 0) {
         if (a.bf16 && a.d == 64) attend<__bf16, 64>(a, v, s);
         else if (a.bf16) attend<__bf16, 128>(a, v, s);

@@ -154,3 +154,48 @@ def test_dropped_pages_in_front_of_rows_whose_own_page_is_bad(new, past, dtype):
     o, lse = w.attend()
     for rows in ([r for r in range(new) if (past + r) // 64 not in bad], [r for r in range(new) if (past + r) // 64 in bad]):
         check_with_bad_pages(w, o, lse, bad + gone, EPS, torch.tensor(rows, device="cuda"))
+
+
+# ---- rows that nothing writes --------------------------------------------------------------
+
+def poisoned(*shapes):
+    """Memory of these shapes given back to the allocator full of 7."""
+    for shape, t in shapes:
+        torch.full(shape, 7.0, dtype=t, device="cuda")
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("new,past,extra,max_new", [
+    ([40, 1, 7], [100, 64, 3], 9, 40), ([1, 1], [100, 64], 5, 1), ([3, 80, 1, 17], [100, 10, 200, 0], 0, 3),
+    ([3, 80, 1, 17], [100, 10, 200, 0], 300, 3), ([0, 5], [64, 1], 2, 5), ([0, 0], [64, 0], 70, 1)])
+def test_rows_that_nothing_attends_for_are_empty(new, past, extra, max_new, dtype):
+    """Rows behind the last sequence, and those of a sequence with more than max_new of them where only
+    single tokens are expected: O = 0 and lse = -inf in outputs that the call makes itself."""
+    w = World(new, past, 4, 2, 64, dtype, seed=31, extra_rows=extra)
+    w.fill_past()
+    w.append()
+    T, n = w.T, sum(new)
+    assert T == n + extra
+    flags = torch.zeros((len(new), 4), dtype=torch.int32, device="cuda")
+    for kw in ({}, {"flags": flags}):
+        poisoned(((T, 4, 64), dtype), ((T, 4), torch.float32))
+        o, lse = w.attend(max_new=max_new, **kw)
+        on = torch.zeros(T, dtype=torch.bool, device="cuda")
+        at = 0
+        for s, m in enumerate(new):
+            if m <= 16 // 2 or max_new > 16 // 2:         # (few rows: 16 with those of two heads per key head)
+                on[at:at + m] = True
+                w.check(o, lse, seqs=[s])
+            at += m
+        assert not o[~on].any() and (lse[~on] == -math.inf).all()
+    assert [bool(f & ops.FLAG_MAX_NEW) for f in flags[:, 0].tolist()] == [m > 8 and max_new <= 8 for m in new]
+
+
+def test_no_sequence_at_all():
+    w = World([4], [10], 2, 2, 64, BF, seed=32)
+    q = w.packed("q")
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    poisoned(((4, 2, 64), BF), ((4, 2), torch.float32))
+    o, lse = w.cache.attend(q, ints(0), none, w.table[:0], 1)
+    assert not o.any() and (lse == -math.inf).all()

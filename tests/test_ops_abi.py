@@ -228,3 +228,13 @@ def test_workspace_sizes_of_empty_calls():
 def test_operator_timing_without_launches():
     acp.acp_timing_reset()
     assert ops.acp_op_timing_read() == {n: (0, 0.0) for n in ops.OP_NAMES}
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(q=0), acp.ACP_EINVAL), (dict(O=8), acp.ACP_EINVAL), (dict(eps=1.0), acp.ACP_EINVAL),
+    (dict(ws=0), acp.ACP_EINVAL), (dict(ws_bytes=16), acp.ACP_EWORKSPACE), (dict(d=80), acp.ACP_EUNSUPPORTED),
+    (dict(T=0, N=0, past=0, table=0, q=0, O=0), acp.ACP_OK),
+])
+def test_attention_with_filled_rows_refuses_the_same(kw, status, monkeypatch):
+    monkeypatch.setattr(ops.lib(), "fox_attn_paged", ops.lib().fox_attn_paged_filled)
+    assert _attend(**kw) == status
