@@ -163,7 +163,7 @@ acp_status acp_paged_append(const void* k, const int64_t* k_strides, const void*
  *        max_new bounds cu[s + 1] - cu[s] and max_len past[s] plus that; they choose
  *        the division of the work and size the workspace.  The rows of a sequence with
  *        more than max_new may be left as they are (flag bit 7 says they were); max_len is a
- *        hint that any value may have.
+ *        hint, any value from 0 to 2^31: results stay right where it is too small or too large.
  *   out: O [T, H, d] dt, lse [T, H] float, contiguous; a row all of whose keys were
  *        left out by bad pages gets O = 0, lse = -inf; c_i counts as 0 where the row's own
  *        page is bad.

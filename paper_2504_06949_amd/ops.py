@@ -414,8 +414,8 @@ class PagedCache:
     def attend(self, q, cu, past, table, max_new: int, max_len: int | None = None, gamma_q=None,
                gamma_k=None, eps: float = 0.0, L_max: int = 131072, out=None, flags=None):
         """(O [T, H, d], lse [T, H]) of the new rows q [T, H, d], after append() of the same
-        rows.  max_new bounds a sequence's new rows; max_len (64 W by default) its length.
-        Rows from cu[N] on, and those of a sequence with more than max_new (flags reports it) that
+        rows.  max_new bounds a sequence's new rows; max_len (by default the table's, at most 2^31)
+        its length, as a hint.  Rows from cu[N] on, and those of a sequence with more than max_new (flags reports it) that
         are not attended for, get O = 0 and lse = -inf, and in `out` stay as they are.
         eps > 0 prunes with gamma_q [H], gamma_k [Hk] float32, for sequences up to L_max."""
         ts = (q, cu, past, table, self.buffer)
@@ -440,7 +440,7 @@ class PagedCache:
                     or o.get_device() != dev or lse.get_device() != dev:
                 raise ValueError("out must be contiguous (O [T, H, d], lse [T, H])")
         if max_len is None:
-            max_len = PAGE * W
+            max_len = min(PAGE * W, 1 << 31)
         need = _sz(0)
         acp._check(lib().acp_paged_workspace_size(T, N, self.H, self.Hk, self.d, self.dt, max_new, max_len,
                                                   ctypes.byref(need)))

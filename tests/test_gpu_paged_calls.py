@@ -199,3 +199,13 @@ def test_no_sequence_at_all():
     poisoned(((4, 2, 64), BF), ((4, 2), torch.float32))
     o, lse = w.cache.attend(q, ints(0), none, w.table[:0], 1)
     assert not o.any() and (lse == -math.inf).all()
+
+
+def test_a_table_as_wide_as_positions_go():
+    """The default max_len of a table of more than 2^31 positions is within its range."""
+    w = World([2, 20], [70, 3], 2, 2, 64, BF, seed=34)
+    w.fill_past()
+    w.append()
+    wide = torch.full((2, (1 << 25) + 3), -1, dtype=torch.int32, device="cuda")
+    wide[:, :w.table.shape[1]] = w.table
+    w.check(*w.cache.attend(w.packed("q"), w.cu, w.past_t, wide, 20, gamma_q=w.gq, gamma_k=w.gk, eps=EPS, L_max=4096))
