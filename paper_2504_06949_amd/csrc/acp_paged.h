@@ -8,6 +8,7 @@ namespace acp {
 
 constexpr int kFlagPage = 64;      // a page number out of range or a table too narrow
 constexpr int kFlagMaxNew = 128;   // a sequence brings more rows than max_new
+constexpr int kFlagScales = 256;   // the weights of a row left the range that the scales promise
 
 // Rows and positions of a sequence, confined to the arrays of the call whatever cu and
 // past hold.

@@ -346,8 +346,8 @@ __device__ __forceinline__ const PagedArgs& late_args() {
     typedef const __attribute__((address_space(4))) char* KernargPtr;
     return *(const PagedArgs*)((KernargPtr)__builtin_amdgcn_kernarg_segment_ptr() + late_zero());
 }
-__device__ __forceinline__ void report(const PagedArgs& a, int s, int h, int lane) {
-    if (a.flags && lane == 0) atomicOr(a.flags + (int64_t)(s + late_zero()) * a.H + h, kFlagPage);
+__device__ __forceinline__ void report(const PagedArgs& a, int s, int h, int lane, int flag = kFlagPage) {
+    if (a.flags && lane == 0) atomicOr(a.flags + (int64_t)(s + late_zero()) * a.H + h, flag);
 }
 
 // Long item `id`, by a wave
@@ -946,6 +946,10 @@ void paged_long_kernel(PagedArgs, Work work, float kscale) {
             const float l = over_groups(blk.l[qt]);
             const int r = o0 + 16 * qt + r16;
             if (r >= rows) continue;
+            // (with a bound that holds: at least e^(-64) of the row's own key, at most 2^31 keys of
+            // e^(2 kFixedMax - 64) = 2^58)
+            const int own = (p0 + r) >> 6;
+            if (fixed && (!(l <= 0x1p92f) || (l < 0x1p-96f && own >= nb && own <= ne))) report(a, s, h, g, kFlagScales);
             if (nb <= ne && sm.marked) add_marks<D>(blk.acc[qt], sm.inf[r], g);
             if (taken == it.pages) put_row<T, D>(a, it.t0 + r, h, blk.acc[qt], blk.max_logit(qt), l, g);
             else put_part<D, kRows>(slot, r, blk.acc[qt], blk.max_logit(qt), l, g);

@@ -37,6 +37,7 @@ HEADER = os.path.join(os.path.dirname(acp.HEADER), "acp_ops.h")
 PAGE = 64                    # positions per page
 FLAG_BAD_PAGE = 64
 FLAG_MAX_NEW = 128
+FLAG_SCALES = 256
 
 OP_NAMES = ("norm", "norm_bwd", "rotary", "append", "attend")
 _LAYOUTS = {"half": 0, "interleaved": 1}
@@ -417,7 +418,10 @@ class PagedCache:
         rows.  max_new bounds a sequence's new rows; max_len (by default the table's, at most 2^31)
         its length, as a hint.  Rows from cu[N] on, and those of a sequence with more than max_new (flags reports it) that
         are not attended for, get O = 0 and lse = -inf, and in `out` stay as they are.
-        eps > 0 prunes with gamma_q [H], gamma_k [Hk] float32, for sequences up to L_max."""
+        eps > 0 prunes with gamma_q [H], gamma_k [Hk] float32, for sequences up to L_max.  The scales
+        must bound the logits, |q.k| / sqrt(d) <= gamma_q gamma_k sqrt(d), as the largest |weight| of
+        QK-normed rows does (times the square of a Rotary's amplitude above 1): they decide what is pruned, and
+        keep the weights of bfloat16 chunks in range (flags reports FLAG_SCALES where they did not)."""
         ts = (q, cu, past, table, self.buffer)
         dev = _device(*ts) if flags is None else _device(*ts, flags)
         N, W = self._sequences(cu, past, table, flags)

@@ -209,3 +209,33 @@ def test_a_table_as_wide_as_positions_go():
     wide = torch.full((2, (1 << 25) + 3), -1, dtype=torch.int32, device="cuda")
     wide[:, :w.table.shape[1]] = w.table
     w.check(*w.cache.attend(w.packed("q"), w.cu, w.past_t, wide, 20, gamma_q=w.gq, gamma_k=w.gk, eps=EPS, L_max=4096))
+
+
+# ---- scales --------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new", [100, 40, 8])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_logits_outside_what_the_scales_allow_are_reported(new, sign, d):
+    """Keys that are the queries or their negatives, and gates of e^-70: a row's logit is all but its own
+    key's, +-U.  At both ends of the bound nothing is reported.  Where the scales allow 1 in place of 110,
+    the weights of a chunk in bfloat16 leave float32's range, which is reported; few rows do without
+    the bound."""
+    U = [8.0, 31.0, 45.0, 51.0]                          # (the reference is U up to 32, 64 - U up to 52)
+    for u in U + [110.0]:
+        scale = math.sqrt(u / math.sqrt(d))
+        w = World([new], [30], 4, 4, d, BF, seed=33, scale=scale, mu=(-70.0, -70.0))
+        w.k = [(sign * t).contiguous() for t in w.q]
+        w.fill_past()
+        w.append()
+        flags = torch.full((1, 4), -1, dtype=torch.int32, device="cuda")
+        o, lse = w.attend(flags=flags)
+        assert not flags.any(), u
+        w.check(o, lse)
+    w.gq[1] = w.gq[3] = 1.0 / (scale * math.sqrt(d))
+    o, lse = w.attend(flags=flags)
+    chunk = 0 if new <= 16 else ops.FLAG_SCALES
+    assert flags.tolist() == [[0, chunk, 0, chunk]]
+    if not chunk:
+        w.check(o, lse)
+    w.attend()                                           # (the same without flags)
