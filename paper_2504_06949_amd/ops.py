@@ -416,12 +416,14 @@ class PagedCache:
                gamma_k=None, eps: float = 0.0, L_max: int = 131072, out=None, flags=None):
         """(O [T, H, d], lse [T, H]) of the new rows q [T, H, d], after append() of the same
         rows.  max_new bounds a sequence's new rows; max_len (by default the table's, at most 2^31)
-        its length, as a hint.  Rows from cu[N] on, and those of a sequence with more than max_new (flags reports it) that
-        are not attended for, get O = 0 and lse = -inf, and in `out` stay as they are.
+        its length, as a hint.  Rows from cu[N] on, and those of a sequence with more than max_new
+        (flags reports it) that are not attended for, get O = 0 and lse = -inf; in `out` they stay
+        as they are.
         eps > 0 prunes with gamma_q [H], gamma_k [Hk] float32, for sequences up to L_max.  The scales
         must bound the logits, |q.k| / sqrt(d) <= gamma_q gamma_k sqrt(d), as the largest |weight| of
-        QK-normed rows does (times the square of a Rotary's amplitude above 1): they decide what is pruned, and
-        keep the weights of bfloat16 chunks in range (flags reports FLAG_SCALES where they did not)."""
+        QK-normed rows does (times the square of a Rotary's amplitude above 1): they decide what is
+        pruned, and keep the weights of bfloat16 chunks in range (flags reports FLAG_SCALES where they
+        did not)."""
         ts = (q, cu, past, table, self.buffer)
         dev = _device(*ts) if flags is None else _device(*ts, flags)
         N, W = self._sequences(cu, past, table, flags)
@@ -449,8 +451,9 @@ class PagedCache:
         acp._check(lib().acp_paged_workspace_size(T, N, self.H, self.Hk, self.d, self.dt, max_new, max_len,
                                                   ctypes.byref(need)))
         ws = self.buffer.new_empty(need.value) if need.value else None
-        _run(lib().fox_attn_paged if out is not None else lib().fox_attn_paged_filled, dev, q.data_ptr(), qs, self.dt, T, N, W, self.P, self.H, self.Hk, self.d,
-             cu.data_ptr(), past.data_ptr(), table.data_ptr(), self.buffer.data_ptr(), self.buffer.numel(),
-             _ptr(gamma_q), _ptr(gamma_k), eps, L_max, max_new, max_len, o.data_ptr(), lse.data_ptr(),
-             _ptr(flags), _ptr(ws), need.value)
+        fn = lib().fox_attn_paged_filled if out is None else lib().fox_attn_paged
+        _run(fn, dev, q.data_ptr(), qs, self.dt, T, N, W, self.P, self.H, self.Hk, self.d, cu.data_ptr(),
+             past.data_ptr(), table.data_ptr(), self.buffer.data_ptr(), self.buffer.numel(), _ptr(gamma_q),
+             _ptr(gamma_k), eps, L_max, max_new, max_len, o.data_ptr(), lse.data_ptr(), _ptr(flags), _ptr(ws),
+             need.value)
         return o, lse

@@ -28,7 +28,7 @@ def ints(*v):
 @pytest.mark.parametrize("gate", [-math.inf, math.nan, math.inf])
 def test_a_sum_of_gates_that_is_not_finite_stays_reported(n, gate):
     """Every later sum of the head inherits it, whatever its own gates."""
-    H = 5                                                # (more heads than a workgroup sums, and not a multiple)
+    H = 5                                       # (more heads than a workgroup sums, and not a multiple)
     cache = ops.PagedCache(60, H, 64, 1)
     table = torch.arange(60, dtype=torch.int32, device="cuda")[None]
     flags = torch.full((1, H), -1, dtype=torch.int32, device="cuda")
@@ -46,8 +46,8 @@ def test_a_sum_of_gates_that_is_not_finite_stays_reported(n, gate):
 # ---- rows whose own page is bad -----------------------------------------------------------
 
 def check_with_bad_pages(w, o, lse, bad, eps, rows, L_max=4096):
-    """O and lse of the given rows of sequence 0 where the pages `bad` are not in the cache: their keys are left out, and
-    c_i is 0 for a row on one.  Tolerances as in World.reference."""
+    """O and lse of the given rows of sequence 0 where the pages `bad` are not in the cache: their keys
+    are left out, and c_i is 0 for a row on one.  Tolerances as in World.reference."""
     p0, L = w.past[0], w.past[0] + w.new[0]
     j = torch.arange(L, device="cuda")
     i = j[p0:, None]
@@ -63,10 +63,12 @@ def check_with_bad_pages(w, o, lse, bad, eps, rows, L_max=4096):
         decay = torch.where(here[p0:], c[p0:], 0.0)[:, None] - c[None]
         seen = (j[None] <= i) & here[None]
         if eps > 0:
-            delta = -(2 * float(w.gq[h].double() * w.gk[hk].double()) * math.sqrt(w.d) + math.log(L_max) - math.log(eps))
+            u = float(w.gq[h].double() * w.gk[hk].double()) * math.sqrt(w.d)
+            delta = -(2 * u + math.log(L_max) - math.log(eps))
             last = (j // 64 * 64 + 63).clamp(max=L - 1)
             seen &= (j // 64)[None] == i // 64
-            seen |= (j[None] // 64 < i // 64) & here[None] & (decay.gather(1, last[None].expand_as(decay)) >= delta)
+            kept = decay.gather(1, last[None].expand_as(decay)) >= delta
+            seen |= (j[None] // 64 < i // 64) & here[None] & kept
         x = torch.where(seen, q @ k.t() / math.sqrt(w.d) + decay, -math.inf)
         top = x.amax(1, keepdim=True)
         p = torch.exp(x - top)
@@ -84,7 +86,8 @@ def check_with_bad_pages(w, o, lse, bad, eps, rows, L_max=4096):
         go, gl = o[rows, h].double(), lse[rows, h].double()
         ro, to, reached, rl, tl = (x[rows] for x in (ro, to, reached, rl, tl))
         assert torch.equal(torch.isfinite(go), ~reached), (h, "which are finite")
-        assert ((go - ro).abs() / to)[~reached].max() <= 1, (h, "O", float(((go - ro).abs() / to)[~reached].max()))
+        off = ((go - ro).abs() / to)[~reached].max()
+        assert off <= 1, (h, "O", float(off))
         assert ((gl - rl).abs() / tl).max() <= 1, (h, "lse", float(((gl - rl).abs() / tl).max()))
 
 
@@ -152,8 +155,9 @@ def test_dropped_pages_in_front_of_rows_whose_own_page_is_bad(new, past, dtype):
     gone = list(range(130))
     w.table[0, gone + bad] = -1
     o, lse = w.attend()
-    for rows in ([r for r in range(new) if (past + r) // 64 not in bad], [r for r in range(new) if (past + r) // 64 in bad]):
-        check_with_bad_pages(w, o, lse, bad + gone, EPS, torch.tensor(rows, device="cuda"))
+    on_bad = torch.tensor([(past + r) // 64 in bad for r in range(new)], device="cuda")
+    for rows in (on_bad, ~on_bad):
+        check_with_bad_pages(w, o, lse, bad + gone, EPS, rows)
 
 
 # ---- rows that nothing writes --------------------------------------------------------------
@@ -184,7 +188,7 @@ def test_rows_that_nothing_attends_for_are_empty(new, past, extra, max_new, dtyp
         on = torch.zeros(T, dtype=torch.bool, device="cuda")
         at = 0
         for s, m in enumerate(new):
-            if m <= 16 // 2 or max_new > 16 // 2:         # (few rows: 16 with those of two heads per key head)
+            if m <= 8 or max_new > 8:            # (few rows: 16 with those of two heads per key head)
                 on[at:at + m] = True
                 w.check(o, lse, seqs=[s])
             at += m
@@ -208,7 +212,8 @@ def test_a_table_as_wide_as_positions_go():
     w.append()
     wide = torch.full((2, (1 << 25) + 3), -1, dtype=torch.int32, device="cuda")
     wide[:, :w.table.shape[1]] = w.table
-    w.check(*w.cache.attend(w.packed("q"), w.cu, w.past_t, wide, 20, gamma_q=w.gq, gamma_k=w.gk, eps=EPS, L_max=4096))
+    w.table = wide
+    w.check(*w.attend(max_new=20))
 
 
 # ---- scales --------------------------------------------------------------------------------
@@ -239,3 +244,137 @@ def test_logits_outside_what_the_scales_allow_are_reported(new, sign, d):
     if not chunk:
         w.check(o, lse)
     w.attend()                                           # (the same without flags)
+
+
+# ---- call arrays and scratch -----------------------------------------------------------------
+
+class Guarded:
+    """Buffers with a pattern on both sides."""
+
+    def __init__(self):
+        self.all = []
+
+    def __call__(self, nbytes, fill=0x5a):
+        side = 1 << 16
+        whole = torch.full((nbytes + 2 * side,), 0xa5, dtype=torch.uint8, device="cuda")
+        inner = whole[side:side + nbytes]
+        inner.fill_(fill)
+        self.all.append((whole, side, nbytes))
+        return inner
+
+    def check(self):
+        for whole, side, n in self.all:
+            assert (whole[:side] == 0xa5).all() and (whole[side + n:] == 0xa5).all()
+
+
+@pytest.mark.parametrize("max_new", [1, 75])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_call_arrays_of_any_content_touch_nothing_else(dtype, max_new):
+    """cu, past and table of any content: what lies around the cache, the outputs, the flags and the
+    workspace stays, and so do the pages that the table does not name."""
+    H, Hk, d, T, N, W, P = 4, 2, 64, 75, 2, 3, 9
+    dt = acp.ACP_F32 if dtype == F32 else acp.ACP_BF16
+    L = ops.lib()
+    n = ops._sz(0)
+    guard = Guarded()
+    acp._check(L.acp_paged_cache_size(P, H, Hk, d, dt, ops.ctypes.byref(n)))
+    cache = guard(n.value, 0)
+    y = ops.PagedLayout()
+    acp._check(L.acp_paged_offsets(P, H, Hk, d, dt, ops.ctypes.byref(y)))
+    pages = {k: cache[a:b].view(P, -1) for k, a, b in (("k", y.k, y.v), ("v", y.v, y.c), ("c", y.c, y.total))}
+    acp._check(L.acp_paged_workspace_size(T, N, H, Hk, d, dt, max_new, 64 * W, ops.ctypes.byref(n)))
+    ws = guard(n.value)
+    o, lse, flags = guard(T * H * d * (4 if dtype == F32 else 2)), guard(T * H * 4), guard(N * H * 4)
+    g = torch.Generator(device="cuda").manual_seed(35)
+    q = torch.randn((T, H, d), generator=g, device="cuda").to(dtype)
+    kv = torch.randn((T, Hk, d), generator=g, device="cuda").to(dtype)
+    f = torch.full((T, H), -0.5, device="cuda")
+    gq, gk = torch.ones(H, device="cuda"), torch.ones(Hk, device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+    tables = [[[0, 2, 4], [6, 7, 8]], [[-1, P, 4], [-(1 << 31), 7, (1 << 31) - 1]],
+              [[P + 1, -5, 1 << 30], [3, -1, -1]], [[-2, -2, -2], [P, P, P]]]
+    for cu in ([0, 5, 75], [0, 1000, 75], [5, 0, -3], [-7, 200, 100], [80, 90, 95], [0, 0, 0], [0, 1, 2]):
+        for past in ([64, 10], [-5, 1 << 30], [0x7fffffff, 0x7fffffff], [-(1 << 31), 190]):
+            for table in tables:
+                print(f"case: call arrays cu={cu} past={past} table={table} {dtype} {max_new}", flush=True)
+                cu_t, past_t, table_t = ints(*cu), ints(*past), torch.tensor(table, dtype=torch.int32, device="cuda")
+                before = {m: t.clone() for m, t in pages.items()}
+                acp._check(L.acp_paged_append(
+                    kv.data_ptr(), None, kv.data_ptr(), None, f.data_ptr(), None, dt, T, N, W, P, H, Hk, d,
+                    cu_t.data_ptr(), past_t.data_ptr(), table_t.data_ptr(), cache.data_ptr(), cache.numel(),
+                    flags.data_ptr(), stream))
+                named = {p for r in table for p in r}
+                rest = [p for p in range(P) if p not in named]
+                for m, t in pages.items():
+                    assert torch.equal(t[rest], before[m][rest]), m
+                kept = cache.clone()
+                for eps, attend in ((EPS, L.fox_attn_paged), (0.0, L.fox_attn_paged), (EPS, L.fox_attn_paged_filled)):
+                    acp._check(attend(
+                        q.data_ptr(), None, dt, T, N, W, P, H, Hk, d, cu_t.data_ptr(), past_t.data_ptr(),
+                        table_t.data_ptr(), cache.data_ptr(), cache.numel(), gq.data_ptr(), gk.data_ptr(), eps, 4096,
+                        max_new, 64 * W, o.data_ptr(), lse.data_ptr(), flags.data_ptr(), ws.data_ptr(), ws.numel(),
+                        stream))
+                assert torch.equal(cache, kept)
+        guard.check()
+
+
+def test_pages_past_32_bit_offsets():
+    """Every page of the call starts past 2^32 elements of its tensor, and past 2^32 bytes of the gates'."""
+    P = (1 << 32) // (4 * 64 * 128) + 20
+    w = World([1, 40], [200, 70], 4, 4, 128, BF, seed=36, spare=0)
+    first = P - w.P
+    w.table = torch.where(w.table >= 0, first + w.table, w.table)
+    w.cache = ops.PagedCache(P, 4, 128, 4, BF)
+    assert w.P <= 20 and int(w.table[w.table >= 0].min()) * 4 * 64 * 128 >= 1 << 32
+    w.fill_past()
+    w.append()
+    w.check_pages()
+    for eps in (EPS, 0.0):
+        w.check(*w.attend(eps), eps)
+
+
+def test_a_captured_step_stores_and_attends():
+    """Replays with the new rows' slots and the outputs overwritten before each: what the graph leaves is
+    what an eager step of the same contents leaves, pages and outputs."""
+    w = World([1, 1, 30], [500, 63, 100], 4, 2, 64, BF, seed=37)
+    w.fill_past()
+    q, k, v, f = (w.packed(n) for n in "qkvf")
+    pos = torch.cat([torch.arange(p, p + n, device="cuda") for p, n in zip(w.past, w.new)])
+    seq = torch.cat([torch.full((n,), s, device="cuda") for s, n in enumerate(w.new)])
+    page, slot = w.table[seq, pos // 64].long(), pos % 64
+    views = w.cache.views()
+
+    def step():
+        w.cache.append(k, v, f, w.cu, w.past_t, w.table)
+        return w.cache.attend(q, w.cu, w.past_t, w.table, 30, gamma_q=w.gq, gamma_k=w.gk, eps=EPS, L_max=4096)
+
+    def wipe(*outs):
+        for t in views.values():
+            t[page, :, slot] = float("nan")
+        for t in outs:
+            t.fill_(float("nan"))
+
+    wipe()
+    step()
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = step()
+        graphs.append((g, out))
+    for r in range(4):
+        for x in (q, k, v, f):
+            x.copy_(x.roll(1, 0))
+        wipe()
+        want = [t.clone() for t in step()]
+        held = {n: t[page, :, slot].clone() for n, t in views.items()}
+        assert all(torch.isfinite(t).all() for t in held.values()) and torch.isfinite(want[0]).all()
+        for g, out in graphs if r % 2 else graphs[::-1]:
+            wipe(*out)
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            for n, t in views.items():
+                assert torch.equal(t[page, :, slot], held[n]), (r, n)
+            assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1]), r
