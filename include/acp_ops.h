@@ -156,7 +156,7 @@ acp_status acp_paged_append(const void* k, const int64_t* k_strides, const void*
  * must bound the logits, |q.k| / sqrt(d) <= U up to rounding, as those of QK-normed rows do: U also
  * keeps the weights of chunks in bfloat16 in float32's range.  Where it does not (logits some 80 away
  * from what the scales allow) such a row may become infinite, NaN or 0 with lse = -inf; flag bit 8 says
- * that a row of the head did (also where q or k is not finite).  Single tokens and float32 do without.
+ * that a row of the head did (also where q, k or c is not finite).  Single tokens and float32 do without.
  * The entries of pages that no row keeps any more may be set to -1 (and the pages used anew):
  * with eps > 0 the search for a row's first kept page takes an entry out of range for a page
  * that the test leaves out, and with it the pages before it, and reports neither.  An entry

@@ -378,3 +378,41 @@ def test_a_captured_step_stores_and_attends():
             for n, t in views.items():
                 assert torch.equal(t[page, :, slot], held[n]), (r, n)
             assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1]), r
+
+
+@pytest.mark.parametrize("long", [False, True])
+def test_the_most_sequences_of_a_call(long):
+    """65535 sequences without a past, one token each (one has 40, some none), 16 query heads on one key head:
+    the single tokens return their values, with their logit as log-sum-exp."""
+    N, H, d = 65535, 16, 64
+    n = torch.ones(N, dtype=torch.int32, device="cuda")
+    n[5::1000] = 0
+    if long:
+        n[40000] = 40
+    cu = torch.zeros(N + 1, dtype=torch.int32, device="cuda")
+    cu[1:] = torch.cumsum(n, 0)
+    T = int(cu[-1])
+    g = torch.Generator(device="cuda").manual_seed(39)
+    q, k, v = (torch.randn((T, heads, d), generator=g, device="cuda").to(BF) for heads in (H, 1, 1))
+    f = -torch.rand((T, H), generator=g, device="cuda")
+    cache = ops.PagedCache(N, H, d, 1)
+    table = torch.randperm(N, generator=g, device="cuda").to(torch.int32)[:, None]
+    flags = torch.full((N, H), -1, dtype=torch.int32, device="cuda")
+    past = torch.zeros(N, dtype=torch.int32, device="cuda")
+    cache.append(k, v, f, cu, past, table, flags=flags)
+    assert not flags.any()
+    o, lse = cache.attend(q, cu, past, table, 40 if long else 1, flags=flags)
+    assert not flags.any()
+    one = torch.ones(T, dtype=torch.bool, device="cuda")
+    if long:
+        at = int(cu[40000])
+        one[at:at + 40] = False
+        c = f[at:at + 40, 3].double().cumsum(0)
+        x = q[at:at + 40, 3].double() @ k[at:at + 40, 0].double().t() / 8 + c[:, None] - c[None]
+        x = torch.where(torch.ones_like(x).tril() > 0, x, -math.inf)
+        # (a logit of at most 10: 24 e of it; 40 keys: 40 e more)
+        assert (lse[at:at + 40, 3].double() - torch.logsumexp(x, 1)).abs().max() <= 300 * E
+    assert torch.equal(o[one], v[one].expand(-1, H, -1))
+    want = (q.float() * k.float()).sum(-1) / 8
+    # (64 products of float32 size |q k|, in any order)
+    assert ((lse - want)[one].abs() <= 64 * E * ((q.float() * k.float()).abs().sum(-1)[one] / 8 + 1)).all()
