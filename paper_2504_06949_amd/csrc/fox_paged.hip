@@ -6,18 +6,27 @@
 // lane holds one query and eight keys of a 32-key half, the running maximum and sum of the
 // softmax per query, and O^T += V^T P^T.
 //   paged_long_kernel   64 or 128 rows of one head per workgroup, 16 or 32 per wave; the
-//                       waves share the pages in LDS.  Bound by the matrix cores and the
-//                       exponentials, which overlap in part: 8000 rows of 16 heads (4 key heads,
-//                       d = 128, bfloat16) behind 8150 positions take 570 us, 890 TFLOP/s, the
-//                       matrix cores busy 42% of the cycles; 2 x 4096 rows of 12 heads (d = 64)
-//                       behind 4096 take 179 us, 590 TFLOP/s (twice the exponentials per
-//                       product); float32, 2048 rows of 4 heads behind 2048, 79 us, 64 TFLOP/s.
+//                       waves share the pages in LDS.  8000 rows of 16 heads (4 key heads, d =
+//                       128, bfloat16) behind 8150 positions take 560 to 610 us, 830 to 910
+//                       TFLOP/s of kept products: the matrix cores are busy 41% of the cycles and
+//                       overlap the exponentials in part, and 3.3 GB pass the L2s meanwhile (a key
+//                       head's 8 MB of pages are read by 63 tiles of 4 heads), 5.4 to 6 TB/s, near
+//                       the rate of plain reads.  2 x 4096 rows of 12 heads (d = 64) behind 4096
+//                       take 163 us a call in a row of them, 650 TFLOP/s (in a trace, with pauses,
+//                       165 and 12 for the merge of 41 MB of sums); matrix cores busy 30%, 12
+//                       registers of a lane spilled at three waves per SIMD.
+//                       (Not the exponentials alone: the forward without pages has as many per
+//                       product at d = 64 and reaches 860 to 890 TFLOP/s.)  float32, 2048 rows
+//                       of 4 heads behind 2048, 79 us, 64 TFLOP/s, where a large product reaches
+//                       154; matrix cores busy 44%.
 //   paged_short_kernel  the rows of all query heads of a key head, where they are at most
 //                       16 in a sequence (single tokens above all): the waves take different
 //                       pages of the same rows.  Bound by memory: a page is read once for
 //                       all query heads that share it.  8 sequences of 4k to 64k positions, 12
 //                       heads, bfloat16: 51 us for 311 MB, 6.1 TB/s, what plain reads of such
-//                       pages reach.
+//                       pages reach.  16 of 3k to 11k, 32 heads on 4 key heads, d = 128: 47 us for
+//                       207 MB, 4.4 TB/s (339 registers and 133 KB of LDS: one workgroup per CU).
+//                       float32, 8 of 100 to 50k, 12 heads: 81 us for 440 MB, 5.5 TB/s.
 // The kept pages of all (rows, head) items, one after the other, are dealt in equal shares to
 // as many workgroups as the chip holds at a time, whatever lengths and heads they belong to:
 // paged_plan_kernel finds each item's pages, every workgroup adds up where its share lies,
@@ -1387,8 +1396,8 @@ Division divide(const PagedArgs& a) {
     // (rows in equal parts that are long: no sequence is short)
     v.short_on = !v.long_on || (int64_t)a.N * a.max_new != a.T;
     v.long_above = v.short_on ? v.short_max : 0;
-    // (4 x 64 rows behind 4000, 12 heads of 64: 28 us at one, 32 at two; 2 x 4096 rows 179 at
-    // two, 241 at one)
+    // (4 x 64 rows behind 4000, 12 heads of 64: 28 us at one, 32 at two; 2 x 4096 rows behind 4096
+    // 179 at two, 241 at one, on a box slower than the one of the head of this file)
     v.nq = a.max_new > 64 ? 2 : 1;
     const int rows = 64 * v.nq;
     auto take = [&](size_t n) {
